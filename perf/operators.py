@@ -5,8 +5,8 @@ a cache, norm and rotate queries and keys, write keys and values into the cache 
 
     tables   sol_attn_block_tables: pages, block tables, slots and positions from the requests' lengths
     norm     sol_attn_qk_norm_rope: RMS norm of each head of q and k and the position rotation
-    append   sol_attn_kv4_append and sol_attn_kv4_read: keys and values into the cache, and back as the values that are held
-    attend   sol_attn_kv4_attention: softmax attention over the pages of each request
+    append   sol_attn_cache_append and sol_attn_cache_read: keys and values into the cache, and back as the values that are held
+    attend   sol_attn_cache_attention: softmax attention over the pages of each request
 
 A page of the cache holds ``page`` tokens of every key/value head, in units of 16 tokens.  A unit of d channels is 18 d bytes: the codes
 of the keys and of the values (e2m1, the lower channel in the lower four bits) and their scales (e4m3, one for 16 channels).  Keys' codes lie
@@ -254,14 +254,14 @@ def _run_own(s):
                                   layout=sol.SOL_LAYOUT_BHND if c["heads_first"] else sol.SOL_LAYOUT_BNHD)
         return [s["q_out"], s["k_out"]]
     if "handle" not in s:      # what a program keeps: the cache's description and the workspace
-        s["handle"] = sol.Kv4Cache(s["cache"], s["pages"], c["page"], c["kv_heads"], c["d"], c.get("k_exp", 0), c.get("v_exp", 0))
+        s["handle"] = sol.Cache(s["cache"], s["pages"], c["page"], c["kv_heads"], c["d"], c.get("k_exp", 0), c.get("v_exp", 0))
         if c["op"] == "attend":
-            s["workspace"] = sol.make_kv4_workspace(c["requests"], s["max_q"], c["heads"], c["kv_heads"], c["d"])
+            s["workspace"] = sol.make_cache_workspace(s["max_q"], c["heads"], c["kv_heads"], c["d"])
     if c["op"] == "append":
-        sol.sol_attn_kv4_append(s["k"], s["v"], s["slots"], s["handle"])
-        sol.sol_attn_kv4_read(s["handle"], s["slots"], s["k_out"], s["v_out"])
+        sol.sol_attn_cache_append(s["k"], s["v"], s["slots"], s["handle"])
+        sol.sol_attn_cache_read(s["handle"], s["slots"], s["k_out"], s["v_out"])
         return [s["k_out"], s["v_out"]]
-    sol.sol_attn_kv4_attention(s["q"], s["cu"], s["kv"], s["table"], s["handle"], s["out"], s["max_q"], s["workspace"], lse=s["lse"],
+    sol.sol_attn_cache_attention(s["q"], s["cu"], s["kv"], s["table"], s["handle"], s["out"], s["max_q"], s["workspace"], lse=s["lse"],
                                causal=c["causal"])
     return [s["out"], s["lse"]]
 
