@@ -291,6 +291,138 @@ sol_status_t sol_attn_route_materialized(const float* qbar, const float* kc, int
                                          int d, float scale, int policy, float param, float* proxy_map,
                                          int32_t* order, float* tau, int32_t* counts, sol_stream_t stream);
 
+/* ---- A generator's cache of keys and values, held in 4 bits --------------------------------------------------
+ * Chunk-wise generation attends to the tokens of all earlier chunks.  The entry points below hold them in a
+ * paged cache and attend to it, one step after the other on one stream, for a ragged batch of requests:
+ *   sol_attn_block_tables      this step's tokens get pages, slots and positions
+ *   sol_attn_qk_norm_rope      q and k are normed per head and rotated
+ *   sol_attn_cache_append      k and v are written to their slots in 4 bits
+ *   sol_attn_cache_attention   q attends to everything cached (this step's tokens among it)
+ * They need no bound workspace, allocate nothing, never synchronise, may be captured and replayed, and are launched with
+ * programmatic stream serialization like the kernels above.  (The paper has no counterpart: its kernels see whole sequences.)
+ * Index arrays are int32 and 4-byte aligned, everything else 16-byte aligned; strides are in elements; the device pointers
+ * belong to the current device, `stream` too.  Outputs must not overlap inputs or one another unless an entry says so. */
+
+/* 16-bit element types of the entry points below */
+enum { SOL_TYPE_BF16 = 0, SOL_TYPE_FP16 = 1 };
+
+/* Pages, slots and positions of a step's tokens.  Request b has old_lens[b] tokens in the cache and brings new_lens[b]
+ * (negative lengths count as 0).  A page holds page_size tokens.  Pages that a request needs beyond the ceil(old / page_size)
+ * that it has are taken from the top of a stack of free pages, request after request: the j-th page that is taken is
+ * free_pages[count - 1 - j], count = *free_count (at most free_capacity).
+ *
+ *   block_tables  [requests][max_blocks], rows table_stride apart, in / out: page ids in order of position.  Entries of pages
+ *                 that are taken are written (-1 where none was left), the others are left alone
+ *   cu_q          [requests + 1], out: token ranges, the running sum of new_lens
+ *   kv_lens       [requests], out: old + new
+ *   slots         [max_tokens], out: page * page_size + place in it of each new token; -1 where it has no page (none left, a
+ *                 table row that is too short, a negative entry).  Entries from cu_q[requests] on are left as they were
+ *   positions     [max_tokens] or NULL, out: position of each new token in its request
+ *   result        [2], out: pages that are left, tokens that got no slot.  Must not be free_count itself, which every
+ *                 block reads: a caller that loops has two and swaps them.
+ *
+ * Pages are taken for the first max_blocks blocks of a request only.  More new tokens than max_tokens: those behind it have no
+ * slot and are counted in result[1]. */
+typedef struct {
+  const int32_t* old_lens; const int32_t* new_lens;
+  const int32_t* free_pages; const int32_t* free_count;
+  int32_t* block_tables; int32_t* cu_q; int32_t* kv_lens; int32_t* slots; int32_t* positions; int32_t* result;
+  int64_t table_stride;
+  int32_t requests, max_blocks, max_tokens, free_capacity, page_size;
+  sol_stream_t stream;
+} sol_attn_tables_args;
+sol_status_t sol_attn_block_tables(const sol_attn_tables_args* args /* host */);
+
+/* RMS norm of each head of q and k, and the position rotation, in one pass.  For a token at position p and a head x of
+ * d channels: y = x / sqrt(mean(x^2) + eps) * weight; the first `rot` channels of y form rot / 2 pairs, pair i being channels
+ * (i, i + rot / 2), or (2 i, 2 i + 1) when `interleaved`; (a, b) becomes (a cos - b sin, a sin + b cos) with cos[p][i], sin[p][i].
+ * Arithmetic in fp32, one rounding at the end.
+ *
+ *   q, k, q_out, k_out   [batch][tokens][heads][d] in any order of the first three, given by the element strides {batch, token,
+ *                        head} of each; d channels contiguous, strides multiples of 8.  q_out may be q and k_out k, with the same
+ *                        strides.  k may be NULL with Hk = 0 (or q with Hq = 0)
+ *   q_weight, k_weight   fp32 [d], or NULL for ones
+ *   cos, sin             fp32 [table_rows][rot / 2]; not read when rot = 0
+ *   positions            int32 [batch][tokens]; NULL: the index of the token in its batch.  A token whose position is not in
+ *                        [0, table_rows) is left out: its rows of the outputs are left as they were (padding)
+ *
+ * d in {64, 128}; rot a multiple of 16 up to d.  Reads and writes every element once. */
+typedef struct {
+  const void* q; const void* k; void* q_out; void* k_out;
+  int64_t q_stride[3], k_stride[3], q_out_stride[3], k_out_stride[3];
+  const float* q_weight; const float* k_weight; const float* cos; const float* sin; const int32_t* positions;
+  int32_t batch, tokens, Hq, Hk, d, rot, interleaved, table_rows, type;
+  float eps;
+  sol_stream_t stream;
+} sol_attn_norm_args;
+sol_status_t sol_attn_qk_norm_rope(const sol_attn_norm_args* args /* host */);
+
+/* A cache: pages of page_size tokens (16, 32, 64, 128 or 256) of all Hk key / value heads.
+ * 16 channels of a token share a scale s, an e4m3 number; each is held as an e2m1 number c, and stands for
+ * c * s * 2^exp (k_exp for keys, v_exp for values, both in [-64, 64]; 0 suits values around 1: what s can tell apart at
+ * full precision lies between 0.016 and 448).  4.5 bits a value.  c * s has six significant bits at most: bf16 and fp16 hold it
+ * exactly (fp16 within its range).
+ *
+ * Layout: [pages][Hk][page_size / 16] units of 18 d bytes, 16 tokens each (token = 8 half + g, or 8 half + 2 t + e):
+ *   keys' codes      [token 16][d / 2]                    lower channel in the lower four bits
+ *   values' codes    [half 2][g 8][t 4][e 2][d / 16]      channels g d / 8 ...
+ *   keys' scales     [g 8][t 4][half 2][d / 64]           groups t d / 64 ...
+ *   values' scales   [group d / 16][t 4][half 2][e 2]
+ * which is the order in which the lanes of a warp take them for m16n8k16 products, 16 bytes each. */
+typedef struct {
+  void* data;                                   /* device, sol_attn_cache_bytes(), 16-byte aligned */
+  int32_t pages, page_size, Hk, d, k_exp, v_exp;
+} sol_attn_cache;
+/* 0 if the shape is unsupported: d in {64, 128}, page sizes as above, pages * page_size < 2^31, Hk <= 1024 */
+size_t sol_attn_cache_bytes(int pages, int page_size, int Hk, int d);
+
+/* Writes keys and values of `tokens` tokens to their slots.  For 16 channels x, scaled by 2^-exp: s = e4m3(max|x| / 6), at most 448;
+ * c = e2m1(x / s), 0 where s is 0; both to nearest, ties to even, saturating: codes are the same on every run and device.
+ * An element that is not finite is held as 0, and the first scale of its token's keys in that head becomes NaN: reading gives NaN in
+ * the key's first 16 channels, and every query that sees the token gets NaN (others are not touched).
+ *   k, v    [tokens][Hk][d], element strides {token, head}, multiples of 8
+ *   slots   int32 [tokens]; a slot outside [0, pages * page_size) is skipped (padding).  Slots that occur must differ: two tokens
+ *           for one slot leave a mixture of both there */
+sol_status_t sol_attn_cache_append(const sol_attn_cache* cache /* host */, const void* k, const void* v, const int64_t k_stride[2],
+                                   const int64_t v_stride[2], const int32_t* slots, int tokens, int type, sol_stream_t stream);
+
+/* Reads the values that the cache holds for `tokens` slots back into k and v (either may be NULL), layouts as above.  Rows of
+ * slots outside the cache are left as they were. */
+sol_status_t sol_attn_cache_read(const sol_attn_cache* cache /* host */, void* k, void* v, const int64_t k_stride[2],
+                                 const int64_t v_stride[2], const int32_t* slots, int tokens, int type, sol_stream_t stream);
+
+/* Softmax attention of a ragged batch of queries over the cache.  Request b has the queries q[cu_q[b]] ... q[cu_q[b + 1] - 1] and the
+ * first kv_lens[b] tokens of its block table (clamped to max_blocks * page_size).  With `causal`, query i of n sees the first
+ * kv_len - n + i + 1 tokens, else all.  Query head h uses key / value head h / (Hq / Hk).
+ *
+ *   q, out       [tokens][Hq][d], element strides {token, head}, multiples of 8; rows outside the requests are neither read nor written
+ *   lse          fp32 [tokens][Hq] contiguous or NULL, out: natural log of the sum of exp(scale q.k)
+ *   block_tables [requests][max_blocks], rows table_stride apart; tokens of a page outside [0, pages) are not seen
+ *   max_q        the longest request's number of queries: chooses the kernel; a longer one is still computed
+ *   scale        logit scale; <= 0 selects 1/sqrt(d)
+ *   workspace    sol_attn_cache_workspace_bytes(), 1024-byte aligned, zeroed once before its first use; overwritten by every call,
+ *                so calls that share one and overlap on the GPU race
+ *
+ * A query that sees nothing gets zeros and lse = -inf.  The cache's values enter the products unrounded; q is scaled by a power of
+ * two per row to fp16 (exact down to 2^-29 of the row's largest element); weights are rounded to fp16; sums are fp32.  Results
+ * do not depend on the order in which blocks run.  d in {64, 128}, Hq a multiple of Hk, Hq <= 1024. */
+typedef struct {
+  const void* q; void* out; float* lse;
+  int64_t q_stride[2], out_stride[2], table_stride;
+  const int32_t* cu_q; const int32_t* kv_lens; const int32_t* block_tables;
+  sol_attn_cache cache;
+  int32_t tokens, requests, max_blocks, max_q, Hq, type, causal;
+  float scale;
+  void* workspace; size_t workspace_bytes;
+  sol_stream_t stream;
+} sol_attn_cache_args;
+sol_status_t sol_attn_cache_attention(const sol_attn_cache_args* args /* host */);
+size_t sol_attn_cache_workspace_bytes(int max_q, int Hq, int Hk, int d);
+
+/* Synchronises `stream`, returns the status word of a workspace of sol_attn_cache_attention (SOL_OK, or SOL_ERR_DEVICE_TIMEOUT
+ * when a kernel gave up on a bounded wait since the word was last read) and clears it. */
+sol_status_t sol_attn_cache_read_status(void* workspace, sol_stream_t stream);
+
 /* Number of kernels the library has launched since it was loaded (for launch accounting). */
 int64_t sol_attn_launch_count(void);
 

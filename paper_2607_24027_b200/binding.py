@@ -32,6 +32,7 @@ SOL_EST_MOMENTS, SOL_EST_DIAGONAL = 0, 1
 SOL_LAYOUT_BHND, SOL_LAYOUT_BNHD = 0, 1
 SOL_ROUTING_FUSED, SOL_ROUTING_PREPASS = 0, 1
 SOL_ROUTE_TOPK, SOL_ROUTE_TOPP = 0, 1
+SOL_TYPE_BF16, SOL_TYPE_FP16 = 0, 1
 
 EXPORTS = [
     "sol_attn_status_string", "sol_attn_workspace_bytes", "sol_attn_workspace_view",
@@ -39,6 +40,8 @@ EXPORTS = [
     "sol_attn_forward_ex", "sol_attn_forward_host", "sol_attn_read_device_status",
     "sol_attn_launch_count", "sol_attn_thresholds_static", "sol_attn_thresholds_static_max_floats",
     "sol_attn_route_materialized", "sol_attn_thresholds", "sol_attn_debug_set_wait", "sol_attn_route_mask",
+    "sol_attn_block_tables", "sol_attn_qk_norm_rope", "sol_attn_cache_bytes", "sol_attn_cache_append", "sol_attn_cache_read",
+    "sol_attn_cache_attention", "sol_attn_cache_workspace_bytes", "sol_attn_cache_read_status",
 ]
 
 
@@ -68,6 +71,35 @@ class _Args(ctypes.Structure):
         ("estimator", ctypes.c_int32), ("forced_blocks", ctypes.c_void_p),
         ("layout", ctypes.c_int32), ("routing", ctypes.c_int32),
     ]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p)] + [(n, ctypes.c_int32) for n in ("pages", "page_size", "Hk", "d", "k_exp", "v_exp")]
+
+
+class _TablesArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("old_lens", "new_lens", "free_pages", "free_count", "block_tables", "cu_q", "kv_lens",
+                                               "slots", "positions", "result")] + \
+               [("table_stride", ctypes.c_int64)] + \
+               [(n, ctypes.c_int32) for n in ("requests", "max_blocks", "max_tokens", "free_capacity", "page_size")] + \
+               [("stream", ctypes.c_void_p)]
+
+
+class _NormArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "q_out", "k_out")] + \
+               [(n, ctypes.c_int64 * 3) for n in ("q_stride", "k_stride", "q_out_stride", "k_out_stride")] + \
+               [(n, ctypes.c_void_p) for n in ("q_weight", "k_weight", "cos", "sin", "positions")] + \
+               [(n, ctypes.c_int32) for n in ("batch", "tokens", "Hq", "Hk", "d", "rot", "interleaved", "table_rows", "type")] + \
+               [("eps", ctypes.c_float), ("stream", ctypes.c_void_p)]
+
+
+class _CacheArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "out", "lse")] + \
+               [("q_stride", ctypes.c_int64 * 2), ("out_stride", ctypes.c_int64 * 2), ("table_stride", ctypes.c_int64)] + \
+               [(n, ctypes.c_void_p) for n in ("cu_q", "kv_lens", "block_tables")] + [("cache", _Cache)] + \
+               [(n, ctypes.c_int32) for n in ("tokens", "requests", "max_blocks", "max_q", "Hq", "type", "causal")] + \
+               [("scale", ctypes.c_float), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+                ("stream", ctypes.c_void_p)]
 
 
 _lib = None
@@ -117,6 +149,22 @@ def lib() -> ctypes.CDLL:
     L.sol_attn_route_materialized.argtypes = [ctypes.c_void_p] * 2 + [ctypes.c_int] * 5 + [ctypes.c_float, ctypes.c_int,
                                                                                            ctypes.c_float] + \
                                              [ctypes.c_void_p] * 5
+    L.sol_attn_block_tables.restype = ctypes.c_int32
+    L.sol_attn_block_tables.argtypes = [ctypes.POINTER(_TablesArgs)]
+    L.sol_attn_qk_norm_rope.restype = ctypes.c_int32
+    L.sol_attn_qk_norm_rope.argtypes = [ctypes.POINTER(_NormArgs)]
+    L.sol_attn_cache_bytes.restype = ctypes.c_size_t
+    L.sol_attn_cache_bytes.argtypes = [ctypes.c_int] * 4
+    for f in (L.sol_attn_cache_append, L.sol_attn_cache_read):
+        f.restype = ctypes.c_int32
+        f.argtypes = [ctypes.POINTER(_Cache)] + [ctypes.c_void_p] * 2 + [ctypes.POINTER(ctypes.c_int64)] * 2 + \
+                     [ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_void_p]
+    L.sol_attn_cache_attention.restype = ctypes.c_int32
+    L.sol_attn_cache_attention.argtypes = [ctypes.POINTER(_CacheArgs)]
+    L.sol_attn_cache_workspace_bytes.restype = ctypes.c_size_t
+    L.sol_attn_cache_workspace_bytes.argtypes = [ctypes.c_int] * 4
+    L.sol_attn_cache_read_status.restype = ctypes.c_int32
+    L.sol_attn_cache_read_status.argtypes = [ctypes.c_void_p] * 2
     L.sol_attn_debug_set_wait.restype = None
     L.sol_attn_debug_set_wait.argtypes = [ctypes.c_int64, ctypes.c_int32]
     _lib = L
@@ -324,6 +372,188 @@ def sol_attn_debug_set_wait(wait_cycles: int = 0, withhold_tile: int = -1):
     """Testing hook: bound of the kernel's device-side waits (SM clocks, <= 0: default) and the tile per CTA
     whose completion signal is withheld (< 0: none)."""
     lib().sol_attn_debug_set_wait(int(wait_cycles), int(withhold_tile))
+
+
+# ----------------------------------------------------------------------------- cache of keys and values in 4 bits
+_TYPES = {torch.bfloat16: SOL_TYPE_BF16, torch.float16: SOL_TYPE_FP16}
+
+
+def _int32(name, t, *shape, rows_apart=False):
+    """A CUDA int32 tensor of this shape (None: any size); contiguous, or with contiguous rows."""
+    if t.dtype != torch.int32 or not t.is_cuda or t.dim() != len(shape) or any(w is not None and w != h for w, h in zip(shape, t.shape)):
+        raise ValueError(f"{name}: expected a CUDA int32 tensor of shape {list(shape)}")
+    if (t.stride(-1) != 1 and t.shape[-1] > 1) if rows_apart else not t.is_contiguous():
+        raise ValueError(f"{name}: not contiguous")
+    return t.data_ptr()
+
+
+def _table(t, B):
+    """(pointer, distance of its rows, columns) of a block table of B requests."""
+    at = _int32("block_tables", t, B, None, rows_apart=True)
+    return at, t.stride(0) if B > 1 else t.shape[1], t.shape[1]
+
+
+def _heads(name, t, dim):
+    """A CUDA bf16 / fp16 tensor of `dim` dimensions whose channels are contiguous."""
+    if t.dim() != dim or t.dtype not in _TYPES or not t.is_cuda or (t.stride(-1) != 1 and t.shape[-1] > 1):
+        raise ValueError(f"{name}: expected a {dim}-dimensional CUDA bf16 or fp16 tensor with contiguous channels")
+    return t
+
+
+def _one_device(stream, *tensors):
+    """The tensors are on the current device, and the stream is one of it (a C call takes both from there)."""
+    at = torch.cuda.current_device()
+    if any(t is not None and t.device.index != at for t in tensors) or (stream is not None and stream.device.index != at):
+        raise ValueError(f"tensors and stream have to be on the current device ({at})")
+
+
+def sol_attn_block_tables(old_lens, new_lens, free_pages, free_count, block_tables, cu_q, kv_lens, slots, result, page_size,
+                          positions=None, stream=None):
+    """Pages, slots and positions of this step's tokens: int32 tensors ``old_lens``, ``new_lens``, ``kv_lens`` [requests], ``cu_q``
+    [requests + 1], ``block_tables`` [requests, max_blocks], ``slots`` and ``positions`` [max_tokens], ``free_count`` [1], ``result`` [2]."""
+    B = int(old_lens.shape[0])
+    _one_device(stream, old_lens, new_lens, free_pages, free_count, block_tables, cu_q, kv_lens, slots, result, positions)
+    n, (table, table_stride, columns) = int(slots.shape[0]), _table(block_tables, B)
+    a = _TablesArgs(old_lens=_int32("old_lens", old_lens, B), new_lens=_int32("new_lens", new_lens, B),
+                    free_pages=_int32("free_pages", free_pages, None), free_count=_int32("free_count", free_count, 1),
+                    block_tables=table, cu_q=_int32("cu_q", cu_q, B + 1),
+                    kv_lens=_int32("kv_lens", kv_lens, B), slots=_int32("slots", slots, n),
+                    positions=None if positions is None else _int32("positions", positions, n), result=_int32("result", result, 2),
+                    table_stride=table_stride, requests=B, max_blocks=columns, max_tokens=n, free_capacity=int(free_pages.shape[0]),
+                    page_size=int(page_size), stream=_stream(stream))
+    _check(lib().sol_attn_block_tables(ctypes.byref(a)), "sol_attn_block_tables")
+
+
+def sol_attn_qk_norm_rope(q, k, q_out, k_out, cos, sin, positions=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False,
+                          layout=SOL_LAYOUT_BNHD, stream=None):
+    """RMS norm of each head and position rotation of ``q`` and ``k`` (either may be None, with its output): [B, N, H, d], or
+    [B, H, N, d] with ``layout=SOL_LAYOUT_BHND``, bf16 or fp16, any strides that are multiples of 8 with contiguous channels.
+    ``cos``, ``sin``: fp32 [rows, rot / 2], or None for no rotation; ``positions``: int32 [B, N]; weights: fp32 [d]."""
+    x = q if q is not None else k
+    if x is None or (q is None) != (q_out is None) or (k is None) != (k_out is None) or (cos is None) != (sin is None):
+        raise ValueError("expected q, k or both, each with its output, and cos with sin")
+    _one_device(stream, q, k, q_out, k_out, cos, sin, positions, q_weight, k_weight)
+    order = (0, 1, 2) if layout == SOL_LAYOUT_BNHD else (0, 2, 1)
+    B, N, d = int(x.shape[0]), int(x.shape[order[1]]), int(x.shape[-1])
+    strides, heads = {}, {}
+    for name, t, other in (("q", q, q_out), ("k", k, k_out), ("q_out", q_out, q), ("k_out", k_out, k)):
+        strides[name], heads[name] = (0, 0, 0), 0
+        if t is not None:
+            _heads(name, t, 4)
+            if t.shape != other.shape or t.dtype != x.dtype or (t.shape[0], t.shape[order[1]], t.shape[3]) != (B, N, d):
+                raise ValueError(f"{name}: shape or type does not match")
+            strides[name] = tuple(t.stride(i) if t.shape[i] > 1 else 0 for i in order)
+            heads[name] = int(t.shape[order[2]])
+    for name, t, shape in (("cos", cos, None), ("sin", sin, None), ("q_weight", q_weight, (d,)), ("k_weight", k_weight, (d,))):
+        if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or (t.dim() != 2 if shape is None else tuple(t.shape) != shape)):
+            raise ValueError(f"{name}: expected a contiguous CUDA fp32 tensor" + (f" of shape {list(shape)}" if shape else " of two dimensions"))
+    if cos is not None and cos.shape != sin.shape:
+        raise ValueError("cos and sin have different shapes")
+    three = ctypes.c_int64 * 3
+    a = _NormArgs(q=_ptr(q), k=_ptr(k), q_out=_ptr(q_out), k_out=_ptr(k_out), q_stride=three(*strides["q"]),
+                  k_stride=three(*strides["k"]), q_out_stride=three(*strides["q_out"]), k_out_stride=three(*strides["k_out"]),
+                  q_weight=_ptr(q_weight), k_weight=_ptr(k_weight), cos=_ptr(cos), sin=_ptr(sin),
+                  positions=None if positions is None else _int32("positions", positions, B, N), batch=B, tokens=N, Hq=heads["q"],
+                  Hk=heads["k"], d=d, rot=0 if cos is None else 2 * int(cos.shape[1]), interleaved=int(interleaved),
+                  table_rows=0 if cos is None else int(cos.shape[0]), type=_TYPES[x.dtype], eps=float(eps), stream=_stream(stream))
+    _check(lib().sol_attn_qk_norm_rope(ctypes.byref(a)), "sol_attn_qk_norm_rope")
+
+
+@dataclass
+class Cache:
+    """Pages of keys and values held in 4 bits (see ``sol_attn_cache`` in the header)."""
+    data: torch.Tensor           # uint8
+    pages: int
+    page_size: int
+    heads: int                   # key / value heads
+    d: int
+    k_exp: int = 0
+    v_exp: int = 0
+
+    def c(self) -> _Cache:
+        need = sol_attn_cache_bytes(self.pages, self.page_size, self.heads, self.d)
+        if self.data.dtype != torch.uint8 or not self.data.is_cuda or not self.data.is_contiguous() or self.data.numel() < need:
+            raise ValueError(f"cache: expected a contiguous CUDA uint8 tensor of {need} bytes")
+        return _Cache(self.data.data_ptr(), self.pages, self.page_size, self.heads, self.d, self.k_exp, self.v_exp)
+
+
+def sol_attn_cache_bytes(pages, page_size, heads, d) -> int:
+    return int(lib().sol_attn_cache_bytes(pages, page_size, heads, d))
+
+
+def make_cache(pages, page_size, heads, d, k_exp=0, v_exp=0, device="cuda") -> Cache:
+    """Allocate (with torch) an empty cache."""
+    n = sol_attn_cache_bytes(pages, page_size, heads, d)
+    if n == 0:
+        raise SolAttnError(SOL_ERR_UNSUPPORTED_SHAPE, "sol_attn_cache_bytes")
+    return Cache(torch.zeros(n, dtype=torch.uint8, device=device), pages, page_size, heads, d, k_exp, v_exp)
+
+
+def _cache_rows(cache, k, v, slots, stream):
+    _one_device(stream, cache.data, k, v, slots)
+    x = k if k is not None else v
+    if x is None:
+        raise ValueError("expected k, v or both")
+    n, strides = int(slots.shape[0]), []
+    for name, t in (("k", k), ("v", v)):
+        if t is not None and (_heads(name, t, 3).dtype != x.dtype or tuple(t.shape) != (n, cache.heads, cache.d)):
+            raise ValueError(f"{name}: expected shape {[n, cache.heads, cache.d]}, k and v of one type")
+        strides.append((ctypes.c_int64 * 2)(*((0, 0) if t is None else (t.stride(i) if t.shape[i] > 1 else 0 for i in (0, 1)))))
+    return ctypes.byref(cache.c()), _ptr(k), _ptr(v), *strides, _int32("slots", slots, n), n, _TYPES[x.dtype], _stream(stream)
+
+
+def sol_attn_cache_append(k, v, slots, cache: Cache, stream=None):
+    """Write keys and values [tokens, heads, d] (bf16 or fp16, contiguous channels) to their ``slots`` (int32 [tokens])."""
+    if k is None or v is None:
+        raise ValueError("expected k and v")
+    _check(lib().sol_attn_cache_append(*_cache_rows(cache, k, v, slots, stream)), "sol_attn_cache_append")
+
+
+def sol_attn_cache_read(cache: Cache, slots, k_out, v_out, stream=None):
+    """Read what ``slots`` hold into ``k_out`` and ``v_out`` [tokens, heads, d] (either may be None)."""
+    _check(lib().sol_attn_cache_read(*_cache_rows(cache, k_out, v_out, slots, stream)), "sol_attn_cache_read")
+
+
+def sol_attn_cache_workspace_bytes(max_q, heads, kv_heads, d) -> int:
+    return int(lib().sol_attn_cache_workspace_bytes(max_q, heads, kv_heads, d))
+
+
+def make_cache_workspace(max_q, heads, kv_heads, d, device="cuda") -> torch.Tensor:
+    """Allocate (with torch) the zeroed workspace of ``sol_attn_cache_attention``, for up to ``max_q`` queries a request."""
+    n = sol_attn_cache_workspace_bytes(max_q, heads, kv_heads, d)
+    if n == 0:
+        raise SolAttnError(SOL_ERR_UNSUPPORTED_SHAPE, "sol_attn_cache_workspace_bytes")
+    buf = torch.zeros(n + 1024, dtype=torch.uint8, device=device)
+    off = (-buf.data_ptr()) % 1024
+    return buf[off:off + n]
+
+
+def sol_attn_cache_attention(q, cu_q, kv_lens, block_tables, cache: Cache, out, max_q, workspace, lse=None, causal=True, scale=0.0,
+                             stream=None):
+    """Attention of ``q`` [tokens, heads, d] (request b: rows cu_q[b] to cu_q[b + 1]) over the first kv_lens[b] tokens of each
+    request's pages, into ``out`` (as q) and ``lse`` (fp32 [tokens, heads])."""
+    _one_device(stream, q, cu_q, kv_lens, block_tables, cache.data, out, workspace, lse)
+    _heads("q", q, 3), _heads("out", out, 3)
+    n, H, d = (int(x) for x in q.shape)
+    if out.shape != q.shape or out.dtype != q.dtype or d != cache.d:
+        raise ValueError("q and out have to agree in shape and type, and with the cache in d")
+    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or tuple(lse.shape) != (n, H)):
+        raise ValueError("lse: expected a contiguous CUDA fp32 tensor of shape [tokens, heads]")
+    if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace: expected a contiguous CUDA uint8 tensor")
+    B, two = int(kv_lens.shape[0]), ctypes.c_int64 * 2
+    table, table_stride, columns = _table(block_tables, B)
+    a = _CacheArgs(q=_ptr(q), out=_ptr(out), lse=_ptr(lse), q_stride=two(*(q.stride(i) if q.shape[i] > 1 else 0 for i in (0, 1))),
+                   out_stride=two(*(out.stride(i) if out.shape[i] > 1 else 0 for i in (0, 1))),
+                   table_stride=table_stride, cu_q=_int32("cu_q", cu_q, B + 1), kv_lens=_int32("kv_lens", kv_lens, B), block_tables=table,
+                   cache=cache.c(), tokens=n, requests=B, max_blocks=columns, max_q=int(max_q), Hq=H,
+                   type=_TYPES[q.dtype], causal=int(causal), scale=float(scale), workspace=workspace.data_ptr(),
+                   workspace_bytes=workspace.numel(), stream=_stream(stream))
+    _check(lib().sol_attn_cache_attention(ctypes.byref(a)), "sol_attn_cache_attention")
+
+
+def sol_attn_cache_read_status(workspace, stream=None) -> int:
+    return int(lib().sol_attn_cache_read_status(workspace.data_ptr(), _stream(stream)))
 
 
 def mask_words(n_k_blocks: int) -> int:

@@ -1,0 +1,159 @@
+// Block tables, slots and positions of a step's tokens (sol_attn_block_tables).
+//
+// Everything follows from two running sums over the requests, of new tokens and of new pages.  Requests are few beside
+// tokens, so every block forms both sums for itself and fills the tokens that it owns: one launch, no block waits for
+// another.  A page is entered in its request's table by the thread of the first token that it holds.
+#include "cache.cuh"
+
+namespace sol {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTokensPerBlock = 1024;
+
+struct TablesParams {
+  const int32_t *old_lens, *new_lens, *free_pages, *free_count;
+  int32_t *tables, *cu_q, *kv_lens, *slots, *positions, *result;
+  long long table_stride;
+  int requests, max_blocks, max_tokens, free_capacity, page_shift;
+};
+
+struct Sum { long long tokens, pages; };
+__device__ __forceinline__ Sum operator+(Sum a, Sum b) { return {a.tokens + b.tokens, a.pages + b.pages}; }
+
+// Inclusive sum over the block's threads; `total` gets the block's.
+__device__ Sum block_scan(Sum x, Sum* warps, Sum* total) {
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  for (int o = 1; o < 32; o *= 2) {
+    const Sum y{__shfl_up_sync(0xffffffffu, x.tokens, o), __shfl_up_sync(0xffffffffu, x.pages, o)};
+    if (lane >= o) x = x + y;
+  }
+  __syncthreads();                               // (the last call's readers)
+  if (lane == 31) warps[warp] = x;
+  __syncthreads();
+  Sum before{0, 0}, all{0, 0};
+  for (int w = 0; w < kThreads / 32; ++w) {
+    if (w < warp) before = before + warps[w];
+    all = all + warps[w];
+  }
+  *total = all;
+  return before + x;
+}
+
+__device__ __forceinline__ int clamp_int(long long x) { return x > 0x7fffffffLL ? 0x7fffffff : (int)x; }
+
+__global__ void __launch_bounds__(kThreads) block_tables_kernel(const TablesParams p) {
+  __shared__ Sum warps[kThreads / 32];
+  __shared__ long long first[kThreads + 1];      // first token of each request of this round, and one behind
+  __shared__ long long page0[kThreads];          // pages taken before it
+  __shared__ int old_of[kThreads];
+  __shared__ unsigned long long without;
+  kernel_wait();
+  const int mask = (1 << p.page_shift) - 1;
+  const long long lo = (long long)blockIdx.x * kTokensPerBlock;
+  const long long hi = min((long long)p.max_tokens, lo + kTokensPerBlock);
+  const int count = max(0, min(*p.free_count, p.free_capacity));
+  const bool writer = blockIdx.x == 0;           // of what there is one of a request
+  if (threadIdx.x == 0) without = 0;
+  auto pages_of = [&](long long tokens) { return min((tokens + mask) >> p.page_shift, (long long)p.max_blocks); };
+  Sum base{0, 0};
+  for (int r = 0; r < p.requests; r += kThreads) {
+    const int b = r + threadIdx.x;
+    const bool on = b < p.requests;
+    const int o = on ? max(0, p.old_lens[b]) : 0, n = on ? max(0, p.new_lens[b]) : 0;
+    const long long have = pages_of(o), need = pages_of((long long)o + n);
+    Sum total;
+    const Sum end = base + block_scan(Sum{n, need - have}, warps, &total);
+    const long long t0 = end.tokens - n, p0 = end.pages - (need - have);
+    first[threadIdx.x] = t0;
+    if (threadIdx.x == kThreads - 1) first[kThreads] = end.tokens;
+    page0[threadIdx.x] = p0;
+    old_of[threadIdx.x] = o;
+    if (writer && on) {
+      p.cu_q[b] = clamp_int(t0);
+      if (b == p.requests - 1) p.cu_q[p.requests] = clamp_int(end.tokens);
+      p.kv_lens[b] = clamp_int((long long)o + n);
+      // tokens without a slot: of the page that was begun, if it is not there; behind the pages that there were; behind max_tokens
+      const long long got = max(0LL, min(need - have, (long long)count - p0));
+      const long long begun = min((long long)n, min((have << p.page_shift), (long long)o + n) - o);   // < 0: its table is too short
+      long long miss = max(0LL, (long long)o + n - max((have + got) << p.page_shift, (long long)o));
+      if (begun > 0 && p.tables[b * p.table_stride + (o >> p.page_shift)] < 0) miss += begun;
+      const long long kept = max(0LL, min((long long)p.max_tokens - t0, (long long)n));
+      if (kept < n) {                            // (those behind max_tokens have none, whatever their pages)
+        const long long in = max(0LL, o + kept - max((have + got) << p.page_shift, (long long)o));
+        miss = n - kept + in;
+        if (begun > 0 && p.tables[b * p.table_stride + (o >> p.page_shift)] < 0) miss += min(begun, kept);
+      }
+      if (miss) atomicAdd(&without, (unsigned long long)miss);
+    }
+    __syncthreads();
+    const long long from = max(lo, base.tokens), to = min(hi, base.tokens + total.tokens);
+    for (long long t = from + threadIdx.x; t < to; t += kThreads) {
+      int a = 0, z = kThreads;                   // the last request that begins at or before t (empty ones begin where the next does)
+      while (z - a > 1) {
+        const int m = (a + z) / 2;
+        if (first[m] <= t) a = m; else z = m;
+      }
+      const long long pos = old_of[a] + (t - first[a]);
+      const long long j = pos >> p.page_shift, had = pages_of(old_of[a]);
+      long long page = -1;
+      if (j < p.max_blocks) {
+        int32_t* entry = p.tables + (r + a) * p.table_stride + j;
+        if (j < had) {
+          page = *entry;
+        } else {
+          const long long rank = page0[a] + j - had;
+          page = rank < count ? p.free_pages[count - 1 - rank] : -1;
+          if (!(pos & mask)) *entry = (int32_t)page;
+        }
+      }
+      const long long slot = (page << p.page_shift) + (pos & mask);
+      p.slots[t] = page < 0 || slot > 0x7fffffffLL ? -1 : (int32_t)slot;
+      if (p.positions) p.positions[t] = clamp_int(pos);
+    }
+    base = base + total;
+    if (!writer && base.tokens >= hi) break;
+    __syncthreads();
+  }
+  if (writer) {
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      if (p.requests == 0) p.cu_q[0] = 0;
+      p.result[0] = (int32_t)max(0LL, count - base.pages);
+      p.result[1] = clamp_int((long long)without);
+    }
+  }
+}
+
+int shift_of(int page_size) {
+  for (int s = 4; s <= 8; ++s)
+    if (page_size == 1 << s) return s;
+  return -1;
+}
+
+}  // namespace
+}  // namespace sol
+
+extern "C" sol_status_t sol_attn_block_tables(const sol_attn_tables_args* a) {
+  if (!a) return SOL_ERR_INVALID_ARG;
+  if (a->requests < 0 || a->max_tokens < 0 || a->max_blocks <= 0 || a->free_capacity < 0) return SOL_ERR_INVALID_ARG;
+  if (!a->cu_q || !a->result || !a->free_count || a->result == a->free_count || a->result + 1 == a->free_count) return SOL_ERR_INVALID_ARG;
+  if (a->requests > 0 && (!a->old_lens || !a->new_lens || !a->block_tables || !a->kv_lens)) return SOL_ERR_INVALID_ARG;
+  if ((a->max_tokens > 0 && !a->slots) || (a->free_capacity > 0 && !a->free_pages)) return SOL_ERR_INVALID_ARG;
+  if (a->table_stride < a->max_blocks) return SOL_ERR_INVALID_ARG;
+  const int shift = sol::shift_of(a->page_size);
+  if (shift < 0) return SOL_ERR_UNSUPPORTED_SHAPE;
+  for (const void* p : {(const void*)a->old_lens, (const void*)a->new_lens, (const void*)a->free_pages, (const void*)a->free_count,
+                        (const void*)a->block_tables, (const void*)a->cu_q, (const void*)a->kv_lens, (const void*)a->slots,
+                        (const void*)a->positions, (const void*)a->result})
+    if (!sol::cache::aligned(p, 4)) return SOL_ERR_INVALID_ARG;
+  const sol_status_t s = sol::check_device_arch();
+  if (s != SOL_OK) return s;
+  sol::TablesParams p{a->old_lens, a->new_lens, a->free_pages, a->free_count, a->block_tables, a->cu_q, a->kv_lens, a->slots,
+                      a->positions, a->result, a->table_stride, a->requests, a->max_blocks, a->max_tokens, a->free_capacity, shift};
+  const int grid = a->max_tokens > 0 ? sol::ceil_div(a->max_tokens, sol::kTokensPerBlock) : 1;
+  const cudaError_t e = sol::launch_after(sol::block_tables_kernel, dim3(grid), sol::kThreads, 0, 0, 0,
+                                          static_cast<cudaStream_t>(a->stream), p);
+  sol::count_launches(1);
+  return e == cudaSuccess ? SOL_OK : SOL_ERR_CUDA;
+}

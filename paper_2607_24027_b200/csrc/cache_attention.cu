@@ -1,0 +1,606 @@
+// Attention of few queries over the 4-bit cache (sol_attn_cache_attention): single tokens, drafts, short chunks.
+//
+// Per key and head 9 d / 8 bytes are read for 4 d flops a row, so with few rows HBM is the bound, and next the work of
+// widening: at 6.5 TB/s an SM gets 44 numbers a clock.  A warp widens what it read in registers and multiplies with
+// m16n8k16 products whose 16-sided operand is the cache: S^T = K Q^T (16 keys x 8 rows), O^T = V^T P^T (16 channels x 8 rows),
+// so that a group of up to 8 query heads costs one product, and the cache's layout gives every lane what its
+// operands hold: no exchange, no shared memory for K or V beyond the lane's own staging.
+//
+// A block is four warps; each takes 32 of the 128 keys of a step with softmax statistics of its own, and the four are joined
+// when a piece ends.  Steps go by copies of 16 bytes into the lane's own part of a ring, kStages - 1 steps ahead.
+#include <cmath>
+
+#include "cache_attention.cuh"
+
+namespace sol {
+namespace cache {
+namespace {
+
+constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kWarpKeys = 32, kStep = kWarps * kWarpKeys;
+constexpr int kStages = 3;
+constexpr unsigned kAll = 0xffffffffu;
+// Weights are kept as 2^15 e^(x - max): fp16 holds them to 2^-12 down to 2^-29 of the largest, and loses less than 2^-40 below.
+constexpr float kWeightShift = 15.f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+template <int D, int NB>
+struct Cfg {
+  static constexpr int kRows = 8 * NB;
+  static constexpr int kPartFloats = kRows * (D + 2);            // O, then maximum and sum of each row
+  static constexpr int kCodeBytes = D / 8;                       // of a lane, unit and half of the keys or values: 16 or 8
+  static constexpr int kStageBytes = 2 * Unit<D>::kBytes;        // of a warp
+  static constexpr int kRing = kWarps * kStages * kStageBytes;
+  static constexpr int kPad = 4;
+  static constexpr int kJoin = kWarps * kRows * (D + kPad) * 4;  // reuses the ring
+  static constexpr int kSmem = (kRing > kJoin ? kRing : kJoin) + kWarps * kRows * 8;
+};
+
+template <int N>
+__device__ __forceinline__ void copy_async(void* dst, const void* src) {
+  const uint32_t d = static_cast<uint32_t>(__cvta_generic_to_shared(dst));
+  if constexpr (N == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(d), "l"(src), "n"(N) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {     // an 8 x 8 matrix of 16-bit numbers, two of a row per lane
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Sum over the block's threads.
+__device__ long long block_sum(long long x, long long* warps) {
+  for (int o = 16; o; o /= 2) x += __shfl_xor_sync(kAll, x, o);
+  __syncthreads();
+  if (threadIdx.x % 32 == 0) warps[threadIdx.x / 32] = x;
+  __syncthreads();
+  long long s = 0;
+  for (int w = 0; w < kWarps; ++w) s += warps[w];
+  return s;
+}
+
+struct Shared {
+  long long warps[kWarps];
+  long long base;                                // first step of request `start`
+  int start;
+};
+
+template <class T, int D, int NB>
+__global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_kernel(const AttnParams p) {
+  using C = Cfg<D, NB>;
+  using U = Unit<D>;
+  constexpr int kSteps16 = D / 16;               // products of 16 channels; also 16-channel tiles of the values
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ Shared sh;
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, t = lane % 4;
+  float2* stats = reinterpret_cast<float2*>(smem + C::kSmem - kWarps * C::kRows * 8);    // [warp][row]: maximum, sum
+  unsigned char* ring = smem + warp * kStages * C::kStageBytes;
+  kernel_wait();
+
+  // ---- this block's share
+  long long mine = 0;
+  for (int b = tid; b < p.requests; b += kThreads) {
+    const Request r = request_at(p, b);
+    mine += Work(r, p.group, C::kRows, kStep).total(p.Hk);
+  }
+  const long long work = block_sum(mine, sh.warps);
+  const long long blocks = min((long long)gridDim.x, work);
+  if ((long long)blockIdx.x >= blocks) {
+    if (tid == 0) p.records[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    return;
+  }
+  long long w = share_begin(work, blocks, blockIdx.x);
+  const long long w_end = share_begin(work, blocks, blockIdx.x + 1);
+  {
+    long long base = 0;
+    for (int b0 = 0; b0 < p.requests; b0 += kThreads) {
+      const int b = b0 + tid;
+      long long n = 0;
+      if (b < p.requests) n = Work(request_at(p, b), p.group, C::kRows, kStep).total(p.Hk);
+      long long x = n;
+      for (int o = 1; o < 32; o *= 2) {
+        const long long y = __shfl_up_sync(kAll, x, o);
+        if (lane >= o) x += y;
+      }
+      __syncthreads();
+      if (lane == 31) sh.warps[warp] = x;
+      __syncthreads();
+      long long before = 0, all = 0;
+      for (int i = 0; i < kWarps; ++i) { if (i < warp) before += sh.warps[i]; all += sh.warps[i]; }
+      const long long lo = base + before + x - n;
+      if (n > 0 && lo <= w && w < lo + n) { sh.start = b; sh.base = lo; }
+      base += all;
+      if (w < base) break;                       // (the whole block)
+    }
+    __syncthreads();
+  }
+  int b = sh.start;
+  long long base = sh.base;
+  Request r = request_at(p, b);
+  Work wk(r, p.group, C::kRows, kStep);
+  int4 record = make_int4(-1, 0, 0, 0);
+  bool first_piece = true;
+
+  while (w < w_end) {
+    while (w >= base + wk.total(p.Hk)) {         // next request with work
+      base += wk.total(p.Hk);
+      ++b;
+      r = request_at(p, b);
+      wk = Work(r, p.group, C::kRows, kStep);
+    }
+    const long long item = (w - base) / wk.steps;
+    const int head = (int)(item / wk.tiles), tile = (int)(item - (long long)head * wk.tiles);
+    const long long item_begin = base + item * wk.steps, item_end = item_begin + wk.steps;
+    const int s_begin = (int)(w - item_begin), s_end = (int)(min(w_end, item_end) - item_begin);
+    const int rows = r.queries * p.group;
+
+    // ---- the rows' queries as the products' 8-sided operand, scaled by a power of two per row so that fp16 holds them
+    uint32_t qf[NB][kSteps16][2];
+    float sl2[NB][2];                            // of rows 2 t and 2 t + 1
+    int sees[NB][2];                             // keys that they see
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const int row = tile * C::kRows + nb * 8 + g;
+      const bool on = row < rows;
+      const int qi = row / p.group, hq = head * p.group + row - qi * p.group;
+      float x[D / 4], most = 0.f;
+      if (on) {
+        const T* src = (const T*)p.q + (r.first + qi) * p.q_s[0] + hq * p.q_s[1] + t * (D / 4);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+          const uint4 raw = reinterpret_cast<const uint4*>(src)[i];
+          const uint32_t wd[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) { const float2 f = Two<T>::widen(wd[j]); x[8 * i + 2 * j] = f.x; x[8 * i + 2 * j + 1] = f.y; }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < D / 4; ++i) x[i] = 0.f;
+      }
+      bool finite = true;
+#pragma unroll
+      for (int i = 0; i < D / 4; ++i) { most = fmaxf(most, fabsf(x[i])); finite = finite && isfinite(x[i]); }
+      most = fmaxf(most, __shfl_xor_sync(kAll, most, 1));
+      most = fmaxf(most, __shfl_xor_sync(kAll, most, 2));
+      finite = ((__ballot_sync(kAll, finite) >> (4 * g)) & 15u) == 15u;
+      // the largest becomes 2^14 to 2^15
+      const int e = finite && most > 0.f ? (int)((__float_as_uint(most) >> 23) & 255) - 127 : 14;
+      const float up = power2(max(-126, min(127, 14 - e)));
+#pragma unroll
+      for (int s = 0; s < kSteps16; ++s)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) qf[nb][s][j] = bits(__floats2half2_rn(x[4 * s + 2 * j] * up, x[4 * s + 2 * j + 1] * up));
+      const float mine2 = finite ? p.sl2 / up : NAN;             // a row that is not finite gives NaN
+      const int seen = !on ? 0 : p.causal ? max(0, r.keys - r.queries + qi + 1) : r.keys;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        sl2[nb][j] = __shfl_sync(kAll, mine2, (2 * t + j) * 4);
+        sees[nb][j] = __shfl_sync(kAll, seen, (2 * t + j) * 4);
+      }
+    }
+    int least = 0x7fffffff;                      // keys that all rows see (rows that are not there do not matter)
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (tile * C::kRows + nb * 8 + 2 * t + j < rows) least = min(least, sees[nb][j]);
+    least = min(least, __shfl_xor_sync(kAll, least, 1));
+    least = min(least, __shfl_xor_sync(kAll, least, 2));
+
+    float o[NB][kSteps16][4], m[NB][2], l[NB][2];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+      for (int s = 0; s < kSteps16; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[nb][s][i] = 0.f;
+      m[nb][0] = m[nb][1] = -INFINITY;
+      l[nb][0] = l[nb][1] = 0.f;
+    }
+
+    // ---- the steps
+    const size_t page_bytes = (size_t)p.Hk * (((size_t)U::kBytes << p.page_shift) / kUnit);
+    const size_t head_at = (size_t)head * (((size_t)U::kBytes << p.page_shift) / kUnit);
+    const int32_t* table = p.tables + b * p.table_stride;
+    const int units = (r.keys + kUnit - 1) / kUnit;
+    int page_of_lane = -1, pages_from = s_begin;                 // lane i holds the page of unit i % 2 of step pages_from + i / 2
+    auto unit_of = [&](int step, int i) { return step * (kStep / kUnit) + warp * 2 + i; };
+    auto load_pages = [&](int from) {
+      pages_from = from;
+      const int u = unit_of(from + lane / 2, lane % 2);
+      page_of_lane = -1;
+      if (u < units) {
+        const int page = table[u >> (p.page_shift - 4)];
+        if (page >= 0 && page < p.pages) page_of_lane = page;
+      }
+    };
+    load_pages(s_begin);
+    unsigned on_hand = 0;                        // bit 2 (step % kStages) + i: the unit is there
+    auto fetch = [&](int step) {
+      if (step < s_end) {
+        if (step >= pages_from + 16) load_pages(step);
+        const int slot = step % kStages;
+        on_hand &= ~(3u << (2 * slot));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int page = __shfl_sync(kAll, page_of_lane, (step - pages_from) * 2 + i);
+          if (page >= 0) {
+            on_hand |= 1u << (2 * slot + i);
+            const int in_page = unit_of(step, i) & ((1 << (p.page_shift - 4)) - 1);
+            const unsigned char* src = p.data + page * page_bytes + head_at + (size_t)in_page * U::kBytes;
+            unsigned char* dst = ring + slot * C::kStageBytes + i * U::kBytes;
+#pragma unroll
+            for (int x = 0; x < 4; ++x)          // keys' and values' codes, two halves each
+              copy_async<C::kCodeBytes>(dst + (x * 32 + lane) * C::kCodeBytes, src + (x * 32 + lane) * C::kCodeBytes);
+            // scales: d / 16 pieces of 16 bytes, by as many lanes (the lanes that use them wait for the warp)
+            if (lane < D / 8) copy_async<16>(dst + U::kKeyScales + lane * 16, src + U::kKeyScales + lane * 16);
+          }
+        }
+      }
+      copies_commit();
+    };
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) fetch(s_begin + s);
+    for (int step = s_begin; step < s_end; ++step) {
+      copies_wait<kStages - 2>();
+      __syncwarp();
+      const int slot = step % kStages;
+      const unsigned char* stage = ring + slot * C::kStageBytes;
+      const int key0 = step * kStep + warp * kWarpKeys;
+      if (key0 < r.keys) {
+        float s_[NB][2][4];
+        // S^T of 2 x 16 keys
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const unsigned char* unit = stage + i * U::kBytes;
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) s_[nb][i][x] = 0.f;
+          uint32_t code[2][D / 32];              // rows g and g + 8, D / 4 channels each
+          __half2 sc[2][D / 64];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const unsigned char* src = unit + U::kKeys + (h * 32 + lane) * C::kCodeBytes;
+            if constexpr (D == 128) *reinterpret_cast<uint4*>(code[h]) = *reinterpret_cast<const uint4*>(src);
+            else *reinterpret_cast<uint2*>(code[h]) = *reinterpret_cast<const uint2*>(src);
+          }
+          if constexpr (D == 128) {
+            const uint32_t x = *reinterpret_cast<const uint32_t*>(unit + U::kKeyScales + lane * 4);
+            const __half2 a = scales2(x & 0xffff), c = scales2(x >> 16);
+            sc[0][0] = __low2half2(a); sc[0][1] = __high2half2(a); sc[1][0] = __low2half2(c); sc[1][1] = __high2half2(c);
+          } else {
+            const __half2 a = scales2(*reinterpret_cast<const uint16_t*>(unit + U::kKeyScales + lane * 2));
+            sc[0][0] = __low2half2(a); sc[1][0] = __high2half2(a);
+          }
+#pragma unroll
+          for (int s = 0; s < kSteps16; ++s) {
+            uint32_t a[4];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)          // channels 4 s + 2 j, + 1 of the lane's D / 4
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+                a[2 * j + h] = bits(__hmul2(codes2((code[h][s / 2] >> ((s % 2) * 16 + j * 8)) & 0xff), sc[h][s / 4]));
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) mma(s_[nb][i], a[0], a[1], a[2], a[3], qf[nb][s][0], qf[nb][s][1]);
+          }
+        }
+        // logits; the keys that a row does not see
+        const bool there = (on_hand >> (2 * slot) & 3u) == 3u;
+        const bool whole = there && key0 + kWarpKeys <= least;
+        int valid[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) valid[i] = (on_hand >> (2 * slot + i) & 1u) ? min(kUnit, r.keys - key0 - i * kUnit) : 0;
+        bool grown = false;
+        float m_new[NB][2];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                float& x = s_[nb][i][2 * h + j];
+                x *= sl2[nb][j];
+                if (!whole) {
+                  const int k = g + 8 * h;
+                  if (k >= valid[i] || key0 + i * kUnit + k >= sees[nb][j]) x = -INFINITY;
+                }
+                mx = fmaxf(mx, x);
+              }
+            mx = fmaxf(mx, __shfl_xor_sync(kAll, mx, 4));
+            mx = fmaxf(mx, __shfl_xor_sync(kAll, mx, 8));
+            mx = fmaxf(mx, __shfl_xor_sync(kAll, mx, 16));
+            m_new[nb][j] = fmaxf(m[nb][j], mx);
+            grown = grown || m_new[nb][j] > m[nb][j];
+          }
+        if (__any_sync(kAll, grown)) {
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const float f = m_new[nb][j] == -INFINITY ? 1.f : ex2(m[nb][j] - m_new[nb][j]);
+              m[nb][j] = m_new[nb][j];
+              l[nb][j] *= f;
+#pragma unroll
+              for (int s = 0; s < kSteps16; ++s) { o[nb][s][j] *= f; o[nb][s][2 + j] *= f; }
+            }
+        }
+        // weights, and as the second product's 8-sided operand
+        uint32_t pf[NB][2][2];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          float nm[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) nm[j] = kWeightShift - (m[nb][j] == -INFINITY ? 0.f : m[nb][j]);
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const float e0 = ex2(s_[nb][i][2 * h] + nm[0]), e1 = ex2(s_[nb][i][2 * h + 1] + nm[1]);
+              l[nb][0] += e0;
+              l[nb][1] += e1;
+              pf[nb][i][h] = transpose8(bits(__floats2half2_rn(e0, e1)));
+            }
+        }
+        // O^T += V^T P^T
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const unsigned char* unit = stage + i * U::kBytes;
+          uint32_t even[2][D / 64], odd[2][D / 64];              // bytes: two tokens of an even or odd channel
+          __half2 sc[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t a[D / 64], c[D / 64];                       // tokens 8 h + 2 t and + 1, D / 8 channels each
+            const unsigned char* src = unit + U::kValues + (h * 32 + lane) * C::kCodeBytes;
+            if constexpr (D == 128) {
+              const uint4 x = *reinterpret_cast<const uint4*>(src);
+              a[0] = x.x; a[1] = x.y; c[0] = x.z; c[1] = x.w;
+            } else {
+              const uint2 x = *reinterpret_cast<const uint2*>(src);
+              a[0] = x.x; c[0] = x.y;
+            }
+#pragma unroll
+            for (int y = 0; y < D / 64; ++y) {
+              even[h][y] = (a[y] & 0x0f0f0f0fu) | ((c[y] << 4) & 0xf0f0f0f0u);
+              odd[h][y] = ((a[y] >> 4) & 0x0f0f0f0fu) | (c[y] & 0xf0f0f0f0u);
+            }
+          }
+          uint32_t vs = *reinterpret_cast<const uint32_t*>(unit + U::kValueScales + ((D == 128 ? g : g / 2) * 4 + t) * 4);
+          if (valid[i] < kUnit) {                // what no row may see is multiplied by zero
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+              if (2 * t + (y & 1) + 8 * (y >> 1) >= valid[i]) vs &= ~(0xffu << (8 * y));
+          }
+          sc[0] = scales2(vs & 0xffff);
+          sc[1] = scales2(vs >> 16);
+#pragma unroll
+          for (int s = 0; s < kSteps16; ++s) {   // channels g d / 8 + 2 s, + 1
+            const int sh8 = (s % 4) * 8;
+            const uint32_t a0 = bits(__hmul2(codes2((even[0][s / 4] >> sh8) & 0xff), sc[0]));
+            const uint32_t a1 = bits(__hmul2(codes2((odd[0][s / 4] >> sh8) & 0xff), sc[0]));
+            const uint32_t a2 = bits(__hmul2(codes2((even[1][s / 4] >> sh8) & 0xff), sc[1]));
+            const uint32_t a3 = bits(__hmul2(codes2((odd[1][s / 4] >> sh8) & 0xff), sc[1]));
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) mma(o[nb][s], a0, a1, a2, a3, pf[nb][i][0], pf[nb][i][1]);
+          }
+        }
+      }
+      __syncwarp();
+      fetch(step + kStages - 1);
+    }
+    copies_wait<0>();
+
+    // ---- the four warps' results into one
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float x = l[nb][j];
+        x += __shfl_xor_sync(kAll, x, 4);
+        x += __shfl_xor_sync(kAll, x, 8);
+        x += __shfl_xor_sync(kAll, x, 16);
+        if (g == 0) stats[warp * C::kRows + nb * 8 + 2 * t + j] = make_float2(m[nb][j], x);
+      }
+    __syncthreads();                             // (and every warp is done with its ring)
+    float* join = reinterpret_cast<float*>(smem);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int row = nb * 8 + 2 * t + j;
+        float top = -INFINITY;
+        for (int x = 0; x < kWarps; ++x) top = fmaxf(top, stats[x * C::kRows + row].x);
+        const float f = top == -INFINITY ? 1.f : ex2(m[nb][j] - top);
+        float* dst = join + (warp * C::kRows + row) * (D + C::kPad) + g * (D / 8);
+#pragma unroll
+        for (int s = 0; s < kSteps16; ++s)
+          *reinterpret_cast<float2*>(dst + 2 * s) = make_float2(o[nb][s][j] * f, o[nb][s][2 + j] * f);
+      }
+    __syncthreads();
+    const bool begins = s_begin == 0, ends = s_end == wk.steps;
+    float* part = p.parts + (size_t)(2 * blockIdx.x + (first_piece && !begins ? 0 : 1)) * C::kPartFloats;
+    for (int x = tid; x < C::kRows * D; x += kThreads) {
+      const int row = x / D, ch = x - row * D;
+      float top = -INFINITY, sum = 0.f, acc = 0.f;
+      for (int y = 0; y < kWarps; ++y) top = fmaxf(top, stats[y * C::kRows + row].x);
+      for (int y = 0; y < kWarps; ++y) {
+        const float2 st = stats[y * C::kRows + row];
+        sum += st.y * (top == -INFINITY ? 1.f : ex2(st.x - top));
+        acc += join[(y * C::kRows + row) * (D + C::kPad) + ch];
+      }
+      if (begins && ends) {
+        const int full = tile * C::kRows + row;
+        if (full < rows) {
+          const int qi = full / p.group, hq = head * p.group + full - qi * p.group;
+          const float y = sum == 0.f ? 0.f : acc / sum * p.v_scale;
+          T* dst = (T*)p.out + (r.first + qi) * p.o_s[0] + hq * p.o_s[1];
+          dst[ch] = T(y);
+          if (p.lse && ch == 0)
+            p.lse[(size_t)(r.first + qi) * p.Hq + hq] = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(sum) - kWeightShift) * kLn2;
+        }
+      } else {
+        part[x] = acc;
+        if (ch == 0) { part[C::kRows * D + row] = top; part[C::kRows * (D + 1) + row] = sum; }
+      }
+    }
+    if (!begins && ends)                         // the last piece of a cut item: this block's record has it combined
+      record = make_int4((int)owner_of(work, blocks, item_begin), b, head, tile);
+    __syncthreads();
+    first_piece = false;
+    w = item_begin + s_end;
+  }
+  if (tid == 0) p.records[blockIdx.x] = record;
+}
+
+// Joins the pieces of an item that several blocks had: block c of the first kernel had the last one, and blocks records[c].x ... c
+// - 1 the others, each in its second place but for those that had nothing else and began inside (first place).
+constexpr int kCombineRows = 2;
+template <class T, int D, int NB>
+__global__ void __launch_bounds__(D * kCombineRows) cache_combine_kernel(const AttnParams p) {
+  using C = Cfg<D, NB>;
+  kernel_wait();
+  const int c = blockIdx.x;
+  const int4 rec = p.records[c];
+  if (rec.x < 0) return;
+  const int row = blockIdx.y * kCombineRows + threadIdx.x / D, ch = threadIdx.x % D;
+  const Request r = request_at(p, rec.y);
+  const int full = rec.w * C::kRows + row;
+  if (full >= r.queries * p.group) return;
+  float top = -INFINITY, sum = 0.f, acc = 0.f;
+#pragma unroll 4
+  for (int x = rec.x; x <= c; ++x) {
+    const float* part = p.parts + (size_t)(2 * x + (x == rec.x ? 1 : 0)) * C::kPartFloats;
+    const float a = part[row * D + ch], m = part[C::kRows * D + row], l = part[C::kRows * (D + 1) + row];
+    const float m_new = fmaxf(top, m);
+    const float f = m_new == -INFINITY ? 1.f : ex2(top - m_new), f1 = m_new == -INFINITY ? 1.f : ex2(m - m_new);
+    acc = acc * f + a * f1;
+    sum = sum * f + l * f1;
+    top = m_new;
+  }
+  const int qi = full / p.group, hq = rec.z * p.group + full - qi * p.group;
+  T* dst = (T*)p.out + (r.first + qi) * p.o_s[0] + hq * p.o_s[1];
+  dst[ch] = T(sum == 0.f ? 0.f : acc / sum * p.v_scale);
+  if (p.lse && ch == 0)
+    p.lse[(size_t)(r.first + qi) * p.Hq + hq] = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(sum) - kWeightShift) * kLn2;
+}
+
+constexpr int kBlocksPerSm = 4, kMostBlocks = 4 * 160;
+constexpr size_t kRecordsAt = 1024;
+
+template <class T, int D, int NB>
+cudaError_t run(const AttnParams& p, int sms, cudaStream_t stream, int* n) {
+  using C = Cfg<D, NB>;
+  int grid = (NB == 1 ? kBlocksPerSm : kBlocksPerSm - 1) * sms;
+  if (grid > kMostBlocks) grid = kMostBlocks;
+  cudaError_t e = launch_after(cache_attention_kernel<T, D, NB>, dim3(grid), kThreads, C::kSmem, C::kSmem, 0, stream, p);
+  if (e == cudaSuccess) {
+    ++*n;
+    e = launch_after(cache_combine_kernel<T, D, NB>, dim3(grid, C::kRows / kCombineRows), D * kCombineRows, 0, 0, 0, stream, p);
+    if (e == cudaSuccess) ++*n;
+  }
+  return e;
+}
+
+size_t workspace_bytes(int rows, int d) {
+  const size_t r = rows <= 8 ? 8 : 16;
+  return align_up(kRecordsAt + kMostBlocks * sizeof(int4) + 2 * kMostBlocks * r * (d + 2) * sizeof(float), 1024);
+}
+
+sol_status_t check_attention(const sol_attn_cache_args* a) {
+  if (!a) return SOL_ERR_INVALID_ARG;
+  sol_status_t s = check(&a->cache);
+  if (s != SOL_OK) return s;
+  if (a->tokens < 0 || a->requests < 0 || a->max_q <= 0 || a->max_blocks <= 0 || a->Hq <= 0) return SOL_ERR_INVALID_ARG;
+  if (a->type != SOL_TYPE_BF16 && a->type != SOL_TYPE_FP16) return SOL_ERR_INVALID_ARG;
+  if (std::isnan(a->scale) || std::isinf(a->scale) || a->table_stride < a->max_blocks) return SOL_ERR_INVALID_ARG;
+  if (a->Hq > kMaxHeads || a->Hq % a->cache.Hk) return SOL_ERR_UNSUPPORTED_SHAPE;
+  if ((long long)a->tokens * (a->Hq / a->cache.Hk) > 0x7fffffffLL) return SOL_ERR_UNSUPPORTED_SHAPE;
+  if (a->tokens > 0 && (!a->q || !a->out || !aligned(a->q, 16) || !aligned(a->out, 16))) return SOL_ERR_INVALID_ARG;
+  if (!strides_ok(a->q_stride, 2) || !strides_ok(a->out_stride, 2) || !aligned(a->lse, 4)) return SOL_ERR_INVALID_ARG;
+  if (a->requests > 0 && (!a->cu_q || !a->kv_lens || !a->block_tables)) return SOL_ERR_INVALID_ARG;
+  if (!aligned(a->cu_q, 4) || !aligned(a->kv_lens, 4) || !aligned(a->block_tables, 4)) return SOL_ERR_INVALID_ARG;
+  const size_t need = sol_attn_cache_workspace_bytes(a->max_q, a->Hq, a->cache.Hk, a->cache.d);
+  if (!a->workspace || !aligned(a->workspace, 1024) || a->workspace_bytes < need) return SOL_ERR_WORKSPACE;
+  return SOL_OK;
+}
+
+}  // namespace
+}  // namespace cache
+}  // namespace sol
+
+extern "C" {
+
+size_t sol_attn_cache_workspace_bytes(int max_q, int Hq, int Hk, int d) {
+  if (max_q <= 0 || Hq <= 0 || Hk <= 0 || Hq > sol::cache::kMaxHeads || Hq % Hk || (d != 64 && d != 128)) return 0;
+  const long long rows = (long long)max_q * (Hq / Hk);
+  return sol::cache::workspace_bytes(rows > 16 ? 16 : (int)rows, d);
+}
+
+sol_status_t sol_attn_cache_attention(const sol_attn_cache_args* a) {
+  using namespace sol;
+  sol_status_t s = cache::check_attention(a);
+  if (s != SOL_OK) return s;
+  if (a->tokens == 0 || a->requests == 0) return SOL_OK;
+  if ((s = check_device_arch()) != SOL_OK) return s;
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return SOL_ERR_CUDA;
+  cache::AttnParams p{};
+  p.q = a->q; p.out = a->out; p.lse = a->lse;
+  for (int i = 0; i < 2; ++i) { p.q_s[i] = a->q_stride[i]; p.o_s[i] = a->out_stride[i]; }
+  p.table_stride = a->table_stride;
+  p.cu_q = a->cu_q; p.kv_lens = a->kv_lens; p.tables = a->block_tables;
+  p.data = static_cast<const unsigned char*>(a->cache.data);
+  p.tokens = a->tokens; p.requests = a->requests; p.max_blocks = a->max_blocks;
+  p.Hq = a->Hq; p.Hk = a->cache.Hk; p.group = a->Hq / a->cache.Hk; p.causal = a->causal != 0; p.pages = a->cache.pages;
+  p.page_shift = a->cache.page_size == 16 ? 4 : a->cache.page_size == 32 ? 5 : a->cache.page_size == 64 ? 6 : a->cache.page_size == 128 ? 7 : 8;
+  const float scale = a->scale > 0.f ? a->scale : 1.0f / std::sqrt((float)a->cache.d);
+  p.sl2 = std::ldexp(scale * 1.4426950408889634f, a->cache.k_exp);
+  p.v_scale = std::ldexp(1.0f, a->cache.v_exp);
+  char* ws = static_cast<char*>(a->workspace);
+  p.status = reinterpret_cast<int32_t*>(ws);
+  p.records = reinterpret_cast<int4*>(ws + cache::kRecordsAt);
+  p.parts = reinterpret_cast<float*>(ws + cache::kRecordsAt + cache::kMostBlocks * sizeof(int4));
+  const cudaStream_t stream = static_cast<cudaStream_t>(a->stream);
+  int n = 0;
+  auto typed = [&](auto zero) {
+    using T = decltype(zero);
+    const bool eight = (long long)a->max_q * p.group <= 8;
+    if (a->cache.d == 128)
+      return eight ? cache::run<T, 128, 1>(p, sms, stream, &n) : cache::run<T, 128, 2>(p, sms, stream, &n);
+    return eight ? cache::run<T, 64, 1>(p, sms, stream, &n) : cache::run<T, 64, 2>(p, sms, stream, &n);
+  };
+  const cudaError_t e = a->type == SOL_TYPE_BF16 ? typed(__nv_bfloat16{}) : typed(__half{});
+  count_launches(n);
+  return e == cudaSuccess ? SOL_OK : SOL_ERR_CUDA;
+}
+
+sol_status_t sol_attn_cache_read_status(void* workspace, sol_stream_t stream) {
+  if (!workspace) return SOL_ERR_WORKSPACE;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int32_t word = 0;
+  if (cudaMemcpyAsync(&word, workspace, sizeof(word), cudaMemcpyDeviceToHost, st) != cudaSuccess) return SOL_ERR_CUDA;
+  if (cudaMemsetAsync(workspace, 0, sizeof(word), st) != cudaSuccess) return SOL_ERR_CUDA;
+  if (cudaStreamSynchronize(st) != cudaSuccess) return SOL_ERR_CUDA;
+  return word;
+}
+
+}  // extern "C"

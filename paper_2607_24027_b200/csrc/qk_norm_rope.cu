@@ -1,0 +1,159 @@
+// RMS norm of each head of q and k and the position rotation in one pass (sol_attn_qk_norm_rope).
+//
+// Bound by HBM: every element is read and written once.  A lane holds 8 channels (16 bytes) of a head, so d / 8 lanes hold a
+// head and a warp 2 (d = 128) or 4 (d = 64) heads at a time; the partner channels of a pair are in the same lane, or rot / 16
+// lanes further.  A warp keeps to one token, whose cos and sin it reads once for all of its heads.
+#include "cache.cuh"
+
+namespace sol {
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kInFlight = 4;                     // head rows of a lane that are loaded before the first is used
+
+struct NormParams {
+  const void *q, *k;
+  void *q_out, *k_out;
+  long long q_s[3], k_s[3], qo_s[3], ko_s[3];
+  const float *q_weight, *k_weight, *cos, *sin;
+  const int32_t* positions;
+  int batch, tokens, Hq, heads, rot, interleaved, table_rows, per_warp;   // heads: of q and k; per_warp: of them, a warp's share
+  float eps;
+};
+
+template <class T, int D>
+__global__ void __launch_bounds__(kWarps * 32) qk_norm_rope_kernel(const NormParams p) {
+  using cache::Two;
+  constexpr int kLanes = D / 8, kRows = 32 / kLanes;
+  const int lane = threadIdx.x % 32, sub = lane / kLanes, c0 = (lane % kLanes) * 8;
+  const long long token = (long long)blockIdx.x * kWarps + threadIdx.x / 32;
+  kernel_wait();
+  if (token >= (long long)p.batch * p.tokens) return;
+  const int b = (int)(token / p.tokens), n = (int)(token - (long long)b * p.tokens);
+  const int pos = p.positions ? p.positions[token] : n;
+  if (p.rot > 0 && (pos < 0 || pos >= p.table_rows)) return;
+  const int half = p.rot / 2;
+  // cos and sin of this lane's pairs: 8 (partner in another lane), or 4 (both here)
+  const bool turns = c0 < p.rot, upper = !p.interleaved && c0 >= half;
+  const int partner = p.interleaved || !turns ? lane : lane + (upper ? -half : half) / 8;
+  float cs[8], sn[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) { cs[i] = 1.f; sn[i] = 0.f; }
+  if (turns) {
+    const size_t at = (size_t)pos * half + (p.interleaved ? c0 / 2 : (upper ? c0 - half : c0));
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+      if (i == 0 || !p.interleaved) {
+        const float4 x = __ldg(reinterpret_cast<const float4*>(p.cos + at + i)), y = __ldg(reinterpret_cast<const float4*>(p.sin + at + i));
+        cs[i] = x.x; cs[i + 1] = x.y; cs[i + 2] = x.z; cs[i + 3] = x.w;
+        sn[i] = y.x; sn[i + 1] = y.y; sn[i + 2] = y.z; sn[i + 3] = y.w;
+      }
+    }
+  }
+  const int h_end = min(p.heads, ((int)blockIdx.y + 1) * p.per_warp);
+  for (int h0 = blockIdx.y * p.per_warp; h0 < h_end; h0 += kRows * kInFlight) {
+    uint4 raw[kInFlight];
+#pragma unroll
+    for (int u = 0; u < kInFlight; ++u) {
+      const int h = h0 + u * kRows + sub;
+      raw[u] = make_uint4(0, 0, 0, 0);
+      if (h < h_end) {
+        const T* src = h < p.Hq ? (const T*)p.q + b * p.q_s[0] + n * p.q_s[1] + h * p.q_s[2]
+                                : (const T*)p.k + b * p.k_s[0] + n * p.k_s[1] + (h - p.Hq) * p.k_s[2];
+        raw[u] = *reinterpret_cast<const uint4*>(src + c0);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kInFlight; ++u) {
+      const int h = h0 + u * kRows + sub;
+      if (h0 + u * kRows >= h_end) break;        // (the whole warp)
+      const bool is_q = h < p.Hq;
+      const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { const float2 f = Two<T>::widen(w[i]); x[2 * i] = f.x; x[2 * i + 1] = f.y; }
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
+#pragma unroll
+      for (int o = 1; o < kLanes; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      const float r = rsqrtf(sum * (1.f / D) + p.eps);
+      const float* weight = is_q ? p.q_weight : p.k_weight;
+#pragma unroll
+      for (int i = 0; i < 8; i += 4) {
+        const float4 g = weight ? __ldg(reinterpret_cast<const float4*>(weight + c0 + i)) : make_float4(1.f, 1.f, 1.f, 1.f);
+        x[i] *= r * g.x; x[i + 1] *= r * g.y; x[i + 2] *= r * g.z; x[i + 3] *= r * g.w;
+      }
+      if (p.interleaved) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float a = x[2 * i], c = x[2 * i + 1];
+          x[2 * i] = a * cs[i] - c * sn[i];
+          x[2 * i + 1] = a * sn[i] + c * cs[i];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {            // (lanes that do not turn get their own value and sin 0)
+          const float y = __shfl_sync(0xffffffffu, x[i], partner);
+          x[i] = x[i] * cs[i] + (upper ? y : -y) * sn[i];
+        }
+      }
+      if (h < h_end) {
+        T* dst = is_q ? (T*)p.q_out + b * p.qo_s[0] + n * p.qo_s[1] + h * p.qo_s[2]
+                      : (T*)p.k_out + b * p.ko_s[0] + n * p.ko_s[1] + (h - p.Hq) * p.ko_s[2];
+        *reinterpret_cast<uint4*>(dst + c0) = make_uint4(Two<T>::round(x[0], x[1]), Two<T>::round(x[2], x[3]),
+                                                         Two<T>::round(x[4], x[5]), Two<T>::round(x[6], x[7]));
+      }
+    }
+  }
+}
+
+}  // namespace
+}  // namespace sol
+
+extern "C" sol_status_t sol_attn_qk_norm_rope(const sol_attn_norm_args* a) {
+  using sol::cache::aligned;
+  if (!a) return SOL_ERR_INVALID_ARG;
+  if (a->batch < 0 || a->tokens < 0 || a->Hq < 0 || a->Hk < 0 || a->Hq + a->Hk <= 0) return SOL_ERR_INVALID_ARG;
+  if (a->type != SOL_TYPE_BF16 && a->type != SOL_TYPE_FP16) return SOL_ERR_INVALID_ARG;
+  if (!(a->eps >= 0.f) || a->rot < 0 || (a->rot > 0 && (!a->cos || !a->sin || a->table_rows <= 0))) return SOL_ERR_INVALID_ARG;
+  if (a->Hq > sol::cache::kMaxHeads || a->Hk > sol::cache::kMaxHeads || (a->d != 64 && a->d != 128) || a->rot > a->d || a->rot % 16 ||
+      (long long)a->batch * a->tokens > 0x7fffffffLL)
+    return SOL_ERR_UNSUPPORTED_SHAPE;
+  if (a->batch == 0 || a->tokens == 0) return SOL_OK;
+  if ((a->Hq > 0 && (!a->q || !a->q_out)) || (a->Hk > 0 && (!a->k || !a->k_out))) return SOL_ERR_INVALID_ARG;
+  for (const void* p : {a->q, a->k, (const void*)a->q_out, (const void*)a->k_out, (const void*)a->q_weight, (const void*)a->k_weight,
+                        (const void*)a->cos, (const void*)a->sin})
+    if (!aligned(p, 16)) return SOL_ERR_INVALID_ARG;
+  if (!aligned(a->positions, 4)) return SOL_ERR_INVALID_ARG;
+  if ((a->Hq > 0 && !(sol::cache::strides_ok(a->q_stride, 3) && sol::cache::strides_ok(a->q_out_stride, 3))) ||
+      (a->Hk > 0 && !(sol::cache::strides_ok(a->k_stride, 3) && sol::cache::strides_ok(a->k_out_stride, 3))))
+    return SOL_ERR_INVALID_ARG;
+  const sol_status_t s = sol::check_device_arch();
+  if (s != SOL_OK) return s;
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return SOL_ERR_CUDA;
+  sol::NormParams p{};
+  p.q = a->q; p.k = a->k; p.q_out = a->q_out; p.k_out = a->k_out;
+  for (int i = 0; i < 3; ++i) {
+    p.q_s[i] = a->q_stride[i]; p.k_s[i] = a->k_stride[i]; p.qo_s[i] = a->q_out_stride[i]; p.ko_s[i] = a->k_out_stride[i];
+  }
+  p.q_weight = a->q_weight; p.k_weight = a->k_weight; p.cos = a->cos; p.sin = a->sin; p.positions = a->positions;
+  p.batch = a->batch; p.tokens = a->tokens; p.Hq = a->Hq; p.heads = a->Hq + a->Hk;
+  p.rot = a->rot; p.interleaved = a->interleaved != 0; p.table_rows = a->table_rows; p.eps = a->eps;
+  // Few tokens: a token's heads are shared out over warps until every SM has 16, down to one load of a warp.
+  const long long tokens = (long long)a->batch * a->tokens;
+  const int rows = 32 / (a->d / 8);
+  int parts = 1;
+  while (tokens * parts < 16LL * sms && parts * rows < p.heads) parts *= 2;
+  p.per_warp = sol::ceil_div(sol::ceil_div(p.heads, parts), rows) * rows;
+  const dim3 grid((unsigned)((tokens + sol::kWarps - 1) / sol::kWarps), (unsigned)sol::ceil_div(p.heads, p.per_warp));
+  const cudaStream_t stream = static_cast<cudaStream_t>(a->stream);
+  auto run = [&](auto kernel) { return sol::launch_after(kernel, grid, sol::kWarps * 32, 0, 0, 0, stream, p); };
+  const cudaError_t e = a->type == SOL_TYPE_BF16
+      ? (a->d == 128 ? run(sol::qk_norm_rope_kernel<__nv_bfloat16, 128>) : run(sol::qk_norm_rope_kernel<__nv_bfloat16, 64>))
+      : (a->d == 128 ? run(sol::qk_norm_rope_kernel<__half, 128>) : run(sol::qk_norm_rope_kernel<__half, 64>));
+  sol::count_launches(1);
+  return e == cudaSuccess ? SOL_OK : SOL_ERR_CUDA;
+}
