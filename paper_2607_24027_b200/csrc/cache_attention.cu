@@ -7,21 +7,27 @@
 // operands hold: no exchange, no shared memory for K or V beyond the lane's own staging.
 //
 // A block is four warps; each takes 32 of the 128 keys of a step with softmax statistics of its own, and the four are joined
-// when a piece ends.  Steps go by copies of 16 bytes into the lane's own part of a ring, kStages - 1 steps ahead.
+// when a piece ends.  The bytes of a step come by one bulk copy (one for each page, if pages are smaller) into a ring,
+// kStages - 1 steps ahead; the warps issue them in turn, which costs each a quarter of the instructions.  Every wait is bounded.
 #include <cmath>
+#include <type_traits>
 
 #include "cache_attention.cuh"
+#include "fwd_sm100_common.cuh"
 
 namespace sol {
 namespace cache {
 namespace {
 
+using namespace ptx;
+
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kWarpKeys = 32, kStep = kWarps * kWarpKeys;
 constexpr int kStages = 3;
 constexpr unsigned kAll = 0xffffffffu;
-// Weights are kept as 2^15 e^(x - max): fp16 holds them to 2^-12 down to 2^-29 of the largest, and loses less than 2^-40 below.
-constexpr float kWeightShift = 15.f;
+// Weights are 2^(x - m + kShift) with x the logit times log2(e) and m a maximum of earlier keys, which is replaced once a weight would
+// pass 2^kMost: fp16 holds them to 2^-12 down to 2^-25 of the largest, and is off by 2^-36 of it at most below.
+constexpr float kShift = 11.f, kMost = 15.f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 template <int D, int NB>
@@ -29,40 +35,27 @@ struct Cfg {
   static constexpr int kRows = 8 * NB;
   static constexpr int kPartFloats = kRows * (D + 2);            // O, then maximum and sum of each row
   static constexpr int kCodeBytes = D / 8;                       // of a lane, unit and half of the keys or values: 16 or 8
-  static constexpr int kStageBytes = 2 * Unit<D>::kBytes;        // of a warp
-  static constexpr int kRing = kWarps * kStages * kStageBytes;
+  static constexpr int kStageBytes = kStep / kUnit * Unit<D>::kBytes;
+  static constexpr int kRing = kStages * kStageBytes;
   static constexpr int kPad = 4;
   static constexpr int kJoin = kWarps * kRows * (D + kPad) * 4;  // reuses the ring
   static constexpr int kSmem = (kRing > kJoin ? kRing : kJoin) + kWarps * kRows * 8;
 };
 
-template <int N>
-__device__ __forceinline__ void copy_async(void* dst, const void* src) {
-  const uint32_t d = static_cast<uint32_t>(__cvta_generic_to_shared(dst));
-  if constexpr (N == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
-  else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(d), "l"(src), "n"(N) : "memory");
-}
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The same with accumulators that start at zero.
+__device__ __forceinline__ void mma_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+               : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {     // an 8 x 8 matrix of 16-bit numbers, two of a row per lane
   uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
   return r;
 }
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 // Sum over the block's threads.
 __device__ long long block_sum(long long x, long long* warps) {
   for (int o = 16; o; o /= 2) x += __shfl_xor_sync(kAll, x, o);
@@ -75,6 +68,9 @@ __device__ long long block_sum(long long x, long long* warps) {
 }
 
 struct Shared {
+  uint64_t full[kStages], empty[kStages];        // a step has landed; all warps are done with it
+  int abort_flag;
+  int missing;                                   // a page of this piece is not there
   long long warps[kWarps];
   long long base;                                // first step of request `start`
   int start;
@@ -85,12 +81,18 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
   using C = Cfg<D, NB>;
   using U = Unit<D>;
   constexpr int kSteps16 = D / 16;               // products of 16 channels; also 16-channel tiles of the values
-  extern __shared__ __align__(16) unsigned char smem[];
+  extern __shared__ __align__(128) unsigned char smem[];
   __shared__ Shared sh;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, t = lane % 4;
   float2* stats = reinterpret_cast<float2*>(smem + C::kSmem - kWarps * C::kRows * 8);    // [warp][row]: maximum, sum
-  unsigned char* ring = smem + warp * kStages * C::kStageBytes;
+  if (tid == 0) {
+    sh.abort_flag = sh.missing = 0;
+    for (int x = 0; x < kStages; ++x) { mbar_init(&sh.full[x], 1); mbar_init(&sh.empty[x], kWarps); }
+    fence_mbar_init();
+  }
+  __syncthreads();
   kernel_wait();
+  kernel_release();                              // (the joining kernel's blocks find room only as this one's leave)
 
   // ---- this block's share
   long long mine = 0;
@@ -134,7 +136,8 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
   Request r = request_at(p, b);
   Work wk(r, p.group, C::kRows, kStep);
   int4 record = make_int4(-1, 0, 0, 0);
-  bool first_piece = true;
+  bool first_piece = true, ok = true;
+  uint32_t fetches = 0;                          // steps of earlier pieces
 
   while (w < w_end) {
     while (w >= base + wk.total(p.Hk)) {         // next request with work
@@ -202,211 +205,232 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
     least = min(least, __shfl_xor_sync(kAll, least, 1));
     least = min(least, __shfl_xor_sync(kAll, least, 2));
 
-    float o[NB][kSteps16][4], m[NB][2], l[NB][2];
+    // exponents are x + nm, x the logit times log2(e): nm = kShift - (a maximum of the row's earlier keys)
+    float o[NB][kSteps16][4], nm[NB][2], l[NB][2];
+    bool seen[NB][2], fresh = true;              // the row has a maximum; some row has none
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
       for (int s = 0; s < kSteps16; ++s)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[nb][s][i] = 0.f;
-      m[nb][0] = m[nb][1] = -INFINITY;
-      l[nb][0] = l[nb][1] = 0.f;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) { nm[nb][j] = 0.f; l[nb][j] = 0.f; seen[nb][j] = false; }
     }
 
     // ---- the steps
-    const size_t page_bytes = (size_t)p.Hk * (((size_t)U::kBytes << p.page_shift) / kUnit);
-    const size_t head_at = (size_t)head * (((size_t)U::kBytes << p.page_shift) / kUnit);
+    const uint32_t page_bytes = (uint32_t)p.Hk * ((uint32_t)U::kBytes << (p.page_shift - 4));
+    const unsigned char* head_data = p.data + (size_t)head * ((size_t)U::kBytes << (p.page_shift - 4));
     const int32_t* table = p.tables + b * p.table_stride;
     const int units = (r.keys + kUnit - 1) / kUnit;
-    int page_of_lane = -1, pages_from = s_begin;                 // lane i holds the page of unit i % 2 of step pages_from + i / 2
     auto unit_of = [&](int step, int i) { return step * (kStep / kUnit) + warp * 2 + i; };
-    auto load_pages = [&](int from) {
-      pages_from = from;
-      const int u = unit_of(from + lane / 2, lane % 2);
-      page_of_lane = -1;
-      if (u < units) {
-        const int page = table[u >> (p.page_shift - 4)];
-        if (page >= 0 && page < p.pages) page_of_lane = page;
-      }
+    auto page_at = [&](int unit) {               // -1: there is none
+      const int page = unit < units ? table[unit >> (p.page_shift - 4)] : -1;
+      return page < p.pages ? page : -1;
     };
-    load_pages(s_begin);
-    unsigned on_hand = 0;                        // bit 2 (step % kStages) + i: the unit is there
+    // A step is fetched by one warp, the warps in turn: by one copy, or one for each page if pages are smaller, a lane each.
+    const int per = min(kStep / kUnit, 1 << (p.page_shift - 4));               // units of a copy
     auto fetch = [&](int step) {
-      if (step < s_end) {
-        if (step >= pages_from + 16) load_pages(step);
-        const int slot = step % kStages;
-        on_hand &= ~(3u << (2 * slot));
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int page = __shfl_sync(kAll, page_of_lane, (step - pages_from) * 2 + i);
-          if (page >= 0) {
-            on_hand |= 1u << (2 * slot + i);
-            const int in_page = unit_of(step, i) & ((1 << (p.page_shift - 4)) - 1);
-            const unsigned char* src = p.data + page * page_bytes + head_at + (size_t)in_page * U::kBytes;
-            unsigned char* dst = ring + slot * C::kStageBytes + i * U::kBytes;
-#pragma unroll
-            for (int x = 0; x < 4; ++x)          // keys' and values' codes, two halves each
-              copy_async<C::kCodeBytes>(dst + (x * 32 + lane) * C::kCodeBytes, src + (x * 32 + lane) * C::kCodeBytes);
-            // scales: d / 16 pieces of 16 bytes, by as many lanes (the lanes that use them wait for the warp)
-            if (lane < D / 8) copy_async<16>(dst + U::kKeyScales + lane * 16, src + U::kKeyScales + lane * 16);
-          }
+      if (step >= s_end) return;
+      const uint32_t n = fetches + (uint32_t)(step - s_begin), s = n % kStages;
+      if (n >= kStages && !__all_sync(kAll, mbar_wait(&sh.empty[s], (n / kStages - 1) & 1, &sh.abort_flag, p.wait_limit))) {
+        ok = false;
+        return;
+      }
+      uint64_t* bar = &sh.full[s];
+      const int u = step * (kStep / kUnit) + lane * per;
+      if (lane * per < kStep / kUnit && u < units) {
+        const int page = table[u >> (p.page_shift - 4)];
+        if (page >= 0 && page < p.pages) {
+          const uint32_t in_page = (uint32_t)u & ((1u << (p.page_shift - 4)) - 1);
+          const uint32_t bytes = (uint32_t)min(per, units - u) * U::kBytes;
+          mbar_expect_tx(bar, bytes);
+          bulk_load_1d(smem + s * C::kStageBytes + lane * per * U::kBytes, head_data + (size_t)(uint32_t)page * page_bytes + in_page * U::kBytes,
+                       bytes, bar);
+        } else {
+          sh.missing = 1;
         }
       }
-      copies_commit();
-    };
-#pragma unroll
-    for (int s = 0; s < kStages - 1; ++s) fetch(s_begin + s);
-    for (int step = s_begin; step < s_end; ++step) {
-      copies_wait<kStages - 2>();
       __syncwarp();
-      const int slot = step % kStages;
-      const unsigned char* stage = ring + slot * C::kStageBytes;
+      if (lane == 0 && (int)n != p.withhold) mbar_arrive(bar);                 // (a test withholds it)
+    };
+
+    // one step of 2 x 16 keys, all of which all rows see if `Whole`
+    auto work_on = [&](int step, const unsigned char* stage, auto whole) {
+      constexpr bool kWhole = decltype(whole)::value;
       const int key0 = step * kStep + warp * kWarpKeys;
-      if (key0 < r.keys) {
-        float s_[NB][2][4];
-        // S^T of 2 x 16 keys
+      int valid[2];
+      if constexpr (!kWhole) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const unsigned char* unit = stage + i * U::kBytes;
+        for (int i = 0; i < 2; ++i) valid[i] = page_at(unit_of(step, i)) >= 0 ? min(kUnit, r.keys - key0 - i * kUnit) : 0;
+      }
+      float y[NB][2][4];
+      // S^T of 2 x 16 keys
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
+      for (int i = 0; i < 2; ++i) {
+        const unsigned char* unit = stage + i * U::kBytes;
+        uint32_t code[2][D / 32];                // rows g and g + 8, D / 4 channels each
+        __half2 sc[2][D / 64];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) s_[nb][i][x] = 0.f;
-          uint32_t code[2][D / 32];              // rows g and g + 8, D / 4 channels each
-          __half2 sc[2][D / 64];
+        for (int h = 0; h < 2; ++h) {
+          const unsigned char* src = unit + U::kKeys + (h * 32 + lane) * C::kCodeBytes;
+          if constexpr (D == 128) *reinterpret_cast<uint4*>(code[h]) = *reinterpret_cast<const uint4*>(src);
+          else *reinterpret_cast<uint2*>(code[h]) = *reinterpret_cast<const uint2*>(src);
+        }
+        if constexpr (D == 128) {
+          const uint32_t x = *reinterpret_cast<const uint32_t*>(unit + U::kKeyScales + lane * 4);
+          const __half2 a = scales2(x & 0xffff), c = scales2(x >> 16);
+          sc[0][0] = __low2half2(a); sc[0][1] = __high2half2(a); sc[1][0] = __low2half2(c); sc[1][1] = __high2half2(c);
+        } else {
+          const __half2 a = scales2(*reinterpret_cast<const uint16_t*>(unit + U::kKeyScales + lane * 2));
+          sc[0][0] = __low2half2(a); sc[1][0] = __high2half2(a);
+        }
+#pragma unroll
+        for (int w4 = 0; w4 < D / 32; ++w4) {    // channels 8 w4 ... of the lane's D / 4: two products
+          uint32_t a[2][4];
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const unsigned char* src = unit + U::kKeys + (h * 32 + lane) * C::kCodeBytes;
-            if constexpr (D == 128) *reinterpret_cast<uint4*>(code[h]) = *reinterpret_cast<const uint4*>(src);
-            else *reinterpret_cast<uint2*>(code[h]) = *reinterpret_cast<const uint2*>(src);
-          }
-          if constexpr (D == 128) {
-            const uint32_t x = *reinterpret_cast<const uint32_t*>(unit + U::kKeyScales + lane * 4);
-            const __half2 a = scales2(x & 0xffff), c = scales2(x >> 16);
-            sc[0][0] = __low2half2(a); sc[0][1] = __high2half2(a); sc[1][0] = __low2half2(c); sc[1][1] = __high2half2(c);
-          } else {
-            const __half2 a = scales2(*reinterpret_cast<const uint16_t*>(unit + U::kKeyScales + lane * 2));
-            sc[0][0] = __low2half2(a); sc[1][0] = __high2half2(a);
+            codes8(code[h][w4], a[h]);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) a[h][x] = bits(__hmul2(half2_of(a[h][x]), sc[h][w4 / 2]));
           }
 #pragma unroll
-          for (int s = 0; s < kSteps16; ++s) {
-            uint32_t a[4];
+          for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int j = 0; j < 2; ++j)          // channels 4 s + 2 j, + 1 of the lane's D / 4
-#pragma unroll
-              for (int h = 0; h < 2; ++h)
-                a[2 * j + h] = bits(__hmul2(codes2((code[h][s / 2] >> ((s % 2) * 16 + j * 8)) & 0xff), sc[h][s / 4]));
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) mma(s_[nb][i], a[0], a[1], a[2], a[3], qf[nb][s][0], qf[nb][s][1]);
-          }
-        }
-        // logits; the keys that a row does not see
-        const bool there = (on_hand >> (2 * slot) & 3u) == 3u;
-        const bool whole = there && key0 + kWarpKeys <= least;
-        int valid[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) valid[i] = (on_hand >> (2 * slot + i) & 1u) ? min(kUnit, r.keys - key0 - i * kUnit) : 0;
-        bool grown = false;
-        float m_new[NB][2];
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            float mx = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                float& x = s_[nb][i][2 * h + j];
-                x *= sl2[nb][j];
-                if (!whole) {
-                  const int k = g + 8 * h;
-                  if (k >= valid[i] || key0 + i * kUnit + k >= sees[nb][j]) x = -INFINITY;
-                }
-                mx = fmaxf(mx, x);
-              }
-            mx = fmaxf(mx, __shfl_xor_sync(kAll, mx, 4));
-            mx = fmaxf(mx, __shfl_xor_sync(kAll, mx, 8));
-            mx = fmaxf(mx, __shfl_xor_sync(kAll, mx, 16));
-            m_new[nb][j] = fmaxf(m[nb][j], mx);
-            grown = grown || m_new[nb][j] > m[nb][j];
-          }
-        if (__any_sync(kAll, grown)) {
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const float f = m_new[nb][j] == -INFINITY ? 1.f : ex2(m[nb][j] - m_new[nb][j]);
-              m[nb][j] = m_new[nb][j];
-              l[nb][j] *= f;
-#pragma unroll
-              for (int s = 0; s < kSteps16; ++s) { o[nb][s][j] *= f; o[nb][s][2 + j] *= f; }
+            for (int nb = 0; nb < NB; ++nb) {
+              const uint32_t q0 = qf[nb][2 * w4 + x][0], q1 = qf[nb][2 * w4 + x][1];
+              if (w4 == 0 && x == 0) mma_first(y[nb][i], a[0][0], a[1][0], a[0][1], a[1][1], q0, q1);
+              else mma(y[nb][i], a[0][2 * x], a[1][2 * x], a[0][2 * x + 1], a[1][2 * x + 1], q0, q1);
             }
         }
-        // weights, and as the second product's 8-sided operand
-        uint32_t pf[NB][2][2];
+      }
+      // Exponents.  A lane looks at its own four keys of a row, and only if one of the warp's is over the limit are maxima taken.
+      bool over = false;
+      float mx[NB][2];
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          float nm[2];
+      for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) nm[j] = kWeightShift - (m[nb][j] == -INFINITY ? 0.f : m[nb][j]);
+        for (int j = 0; j < 2; ++j) {
+          mx[nb][j] = -INFINITY;
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const float e0 = ex2(s_[nb][i][2 * h] + nm[0]), e1 = ex2(s_[nb][i][2 * h + 1] + nm[1]);
-              l[nb][0] += e0;
-              l[nb][1] += e1;
-              pf[nb][i][h] = transpose8(bits(__floats2half2_rn(e0, e1)));
+              float& x = y[nb][i][2 * h + j];
+              x = fmaf(x, sl2[nb][j], nm[nb][j]);
+              if constexpr (!kWhole)
+                if (g + 8 * h >= valid[i] || key0 + i * kUnit + g + 8 * h >= sees[nb][j]) x = -INFINITY;
+              mx[nb][j] = fmaxf(mx[nb][j], x);
             }
+          over = over || mx[nb][j] > kMost;
         }
-        // O^T += V^T P^T
+      if (__any_sync(kAll, over) || fresh) {
+        fresh = false;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const unsigned char* unit = stage + i * U::kBytes;
-          uint32_t even[2][D / 64], odd[2][D / 64];              // bytes: two tokens of an even or odd channel
-          __half2 sc[2];
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            float top = mx[nb][j];
+            top = fmaxf(top, __shfl_xor_sync(kAll, top, 4));
+            top = fmaxf(top, __shfl_xor_sync(kAll, top, 8));
+            top = fmaxf(top, __shfl_xor_sync(kAll, top, 16));
+            // the largest exponent becomes kShift, if it was above (or is the row's first)
+            const float by = top == -INFINITY ? 0.f : seen[nb][j] ? fmaxf(0.f, top - kShift) : top - kShift;
+            const float f = seen[nb][j] ? ex2(-by) : 1.f;        // (nothing is there yet)
+            seen[nb][j] = seen[nb][j] || top != -INFINITY;
+            fresh = fresh || !seen[nb][j];
+            nm[nb][j] -= by;
+            l[nb][j] *= f;
+#pragma unroll
+            for (int s = 0; s < kSteps16; ++s) { o[nb][s][j] *= f; o[nb][s][2 + j] *= f; }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) { y[nb][i][j] -= by; y[nb][i][2 + j] -= by; }
+          }
+        fresh = __any_sync(kAll, fresh);
+      }
+      // weights, and as the second product's 8-sided operand
+      uint32_t pf[NB][2][2];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            uint32_t a[D / 64], c[D / 64];                       // tokens 8 h + 2 t and + 1, D / 8 channels each
-            const unsigned char* src = unit + U::kValues + (h * 32 + lane) * C::kCodeBytes;
-            if constexpr (D == 128) {
-              const uint4 x = *reinterpret_cast<const uint4*>(src);
-              a[0] = x.x; a[1] = x.y; c[0] = x.z; c[1] = x.w;
-            } else {
-              const uint2 x = *reinterpret_cast<const uint2*>(src);
-              a[0] = x.x; c[0] = x.y;
-            }
-#pragma unroll
-            for (int y = 0; y < D / 64; ++y) {
-              even[h][y] = (a[y] & 0x0f0f0f0fu) | ((c[y] << 4) & 0xf0f0f0f0u);
-              odd[h][y] = ((a[y] >> 4) & 0x0f0f0f0fu) | (c[y] & 0xf0f0f0f0u);
-            }
+            const float e0 = ex2(y[nb][i][2 * h]), e1 = ex2(y[nb][i][2 * h + 1]);
+            l[nb][0] += e0;
+            l[nb][1] += e1;
+            pf[nb][i][h] = transpose8(bits(__floats2half2_rn(e0, e1)));
           }
-          uint32_t vs = *reinterpret_cast<const uint32_t*>(unit + U::kValueScales + ((D == 128 ? g : g / 2) * 4 + t) * 4);
-          if (valid[i] < kUnit) {                // what no row may see is multiplied by zero
+      // O^T += V^T P^T
 #pragma unroll
-            for (int y = 0; y < 4; ++y)
-              if (2 * t + (y & 1) + 8 * (y >> 1) >= valid[i]) vs &= ~(0xffu << (8 * y));
-          }
-          sc[0] = scales2(vs & 0xffff);
-          sc[1] = scales2(vs >> 16);
+      for (int i = 0; i < 2; ++i) {
+        const unsigned char* unit = stage + i * U::kBytes;
+        uint32_t vs = *reinterpret_cast<const uint32_t*>(unit + U::kValueScales + ((D == 128 ? g : g / 2) * 4 + t) * 4);
+        if constexpr (!kWhole) {                 // what no row may see is multiplied by zero
 #pragma unroll
-          for (int s = 0; s < kSteps16; ++s) {   // channels g d / 8 + 2 s, + 1
-            const int sh8 = (s % 4) * 8;
-            const uint32_t a0 = bits(__hmul2(codes2((even[0][s / 4] >> sh8) & 0xff), sc[0]));
-            const uint32_t a1 = bits(__hmul2(codes2((odd[0][s / 4] >> sh8) & 0xff), sc[0]));
-            const uint32_t a2 = bits(__hmul2(codes2((even[1][s / 4] >> sh8) & 0xff), sc[1]));
-            const uint32_t a3 = bits(__hmul2(codes2((odd[1][s / 4] >> sh8) & 0xff), sc[1]));
+          for (int x = 0; x < 4; ++x)
+            if (2 * t + (x & 1) + 8 * (x >> 1) >= valid[i]) vs &= ~(0xffu << (8 * x));
+        }
+        const __half2 sc[2] = {scales2(vs & 0xffff), scales2(vs >> 16)};
+        uint32_t a[2][D / 64], c[2][D / 64];     // tokens 8 h + 2 t and + 1, D / 8 channels each
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) mma(o[nb][s], a0, a1, a2, a3, pf[nb][i][0], pf[nb][i][1]);
+        for (int h = 0; h < 2; ++h) {
+          const unsigned char* src = unit + U::kValues + (h * 32 + lane) * C::kCodeBytes;
+          if constexpr (D == 128) {
+            const uint4 x = *reinterpret_cast<const uint4*>(src);
+            a[h][0] = x.x; a[h][1] = x.y; c[h][0] = x.z; c[h][1] = x.w;
+          } else {
+            const uint2 x = *reinterpret_cast<const uint2*>(src);
+            a[h][0] = x.x; c[h][0] = x.y;
           }
         }
+#pragma unroll
+        for (int w4 = 0; w4 < D / 64; ++w4) {    // channels g d / 8 + 8 w4 ...: four tiles of 16
+          uint32_t v[2][2][4];                   // half, odd channel: two tokens each
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t x = a[h][w4], z = c[h][w4];
+            codes8((x & 0x0f0f0f0fu) | ((z << 4) & 0xf0f0f0f0u), v[h][0]);
+            codes8(((x >> 4) & 0x0f0f0f0fu) | (z & 0xf0f0f0f0u), v[h][1]);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[h][q / 4][q % 4] = bits(__hmul2(half2_of(v[h][q / 4][q % 4]), sc[h]));
+          }
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+              mma(o[nb][4 * w4 + q], v[0][0][q], v[0][1][q], v[1][0][q], v[1][1][q], pf[nb][i][0], pf[nb][i][1]);
+        }
       }
+    };
+
+    if (warp < kStages - 1) fetch(s_begin + warp);
+    uint32_t n = fetches;
+    for (int step = s_begin; ok && step < s_end; ++step, ++n) {
+      const uint32_t s = n % kStages;
+      if (!__all_sync(kAll, mbar_wait(&sh.full[s], (n / kStages) & 1, &sh.abort_flag, p.wait_limit))) { ok = false; break; }
+      const unsigned char* stage = smem + s * C::kStageBytes + warp * 2 * U::kBytes;
+      const int key0 = step * kStep + warp * kWarpKeys;
+      if (key0 + kWarpKeys <= least && !*(volatile int*)&sh.missing) work_on(step, stage, std::true_type{});
+      else if (key0 < r.keys) work_on(step, stage, std::false_type{});
       __syncwarp();
-      fetch(step + kStages - 1);
+      if (lane == 0) mbar_arrive(&sh.empty[s]);
+      // (into the place of the step before this one, which the other warps are done with by now or soon)
+      if ((step - s_begin) % kWarps == warp) fetch(step + kStages - 1);
     }
-    copies_wait<0>();
+    if (!ok && lane == 0) {
+      sh.abort_flag = 1;
+      atomicExch(p.status, (int)SOL_ERR_DEVICE_TIMEOUT);
+    }
+    __syncthreads();
+    if (sh.abort_flag) {                         // a wait ran out: no result, but no copy is left in flight either
+      int never = 0;
+      if (!ok)
+        for (uint32_t x = n; x < n + kStages; ++x) mbar_wait(&sh.full[x % kStages], (x / kStages) & 1, &never, p.wait_limit);
+      if (tid == 0) p.records[blockIdx.x] = make_int4(-1, 0, 0, 0);
+      return;
+    }
+    fetches += (uint32_t)(s_end - s_begin);
 
     // ---- the four warps' results into one
 #pragma unroll
@@ -417,7 +441,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
         x += __shfl_xor_sync(kAll, x, 4);
         x += __shfl_xor_sync(kAll, x, 8);
         x += __shfl_xor_sync(kAll, x, 16);
-        if (g == 0) stats[warp * C::kRows + nb * 8 + 2 * t + j] = make_float2(m[nb][j], x);
+        if (g == 0) stats[warp * C::kRows + nb * 8 + 2 * t + j] = make_float2(seen[nb][j] ? kShift - nm[nb][j] : -INFINITY, x);
       }
     __syncthreads();                             // (and every warp is done with its ring)
     float* join = reinterpret_cast<float*>(smem);
@@ -428,7 +452,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
         const int row = nb * 8 + 2 * t + j;
         float top = -INFINITY;
         for (int x = 0; x < kWarps; ++x) top = fmaxf(top, stats[x * C::kRows + row].x);
-        const float f = top == -INFINITY ? 1.f : ex2(m[nb][j] - top);
+        const float f = top == -INFINITY ? 1.f : seen[nb][j] ? ex2(kShift - nm[nb][j] - top) : 0.f;
         float* dst = join + (warp * C::kRows + row) * (D + C::kPad) + g * (D / 8);
 #pragma unroll
         for (int s = 0; s < kSteps16; ++s)
@@ -454,7 +478,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
           T* dst = (T*)p.out + (r.first + qi) * p.o_s[0] + hq * p.o_s[1];
           dst[ch] = T(y);
           if (p.lse && ch == 0)
-            p.lse[(size_t)(r.first + qi) * p.Hq + hq] = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(sum) - kWeightShift) * kLn2;
+            p.lse[(size_t)(r.first + qi) * p.Hq + hq] = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(sum) - kShift) * kLn2;
         }
       } else {
         part[x] = acc;
@@ -463,6 +487,8 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
     }
     if (!begins && ends)                         // the last piece of a cut item: this block's record has it combined
       record = make_int4((int)owner_of(work, blocks, item_begin), b, head, tile);
+    if (tid == 0) sh.missing = 0;
+    fence_proxy_async_smem();                    // the next copies go where the warps' results were
     __syncthreads();
     first_piece = false;
     w = item_begin + s_end;
@@ -470,36 +496,68 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
   if (tid == 0) p.records[blockIdx.x] = record;
 }
 
-// Joins the pieces of an item that several blocks had: block c of the first kernel had the last one, and blocks records[c].x ... c
-// - 1 the others, each in its second place but for those that had nothing else and began inside (first place).
-constexpr int kCombineRows = 2;
+// Joins the pieces of an item that several blocks had: block c of the first kernel had the last piece, blocks records[c].x ... c - 1
+// the others.  The block that had the first piece left it in its second place, the rest in their first.  A row is added up by
+// kJoinWarps / rows warps, four channels (two, d = 64) to a lane.
+constexpr int kJoinWarps = 16;
 template <class T, int D, int NB>
-__global__ void __launch_bounds__(D * kCombineRows) cache_combine_kernel(const AttnParams p) {
+__global__ void __launch_bounds__(32 * kJoinWarps) cache_combine_kernel(const AttnParams p) {
   using C = Cfg<D, NB>;
+  constexpr int kShare = kJoinWarps / C::kRows, kCh = D / 32;
+  __shared__ float joined[kJoinWarps][D + 2];
   kernel_wait();
   const int c = blockIdx.x;
   const int4 rec = p.records[c];
   if (rec.x < 0) return;
-  const int row = blockIdx.y * kCombineRows + threadIdx.x / D, ch = threadIdx.x % D;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, row = warp % C::kRows, share = warp / C::kRows;
   const Request r = request_at(p, rec.y);
   const int full = rec.w * C::kRows + row;
-  if (full >= r.queries * p.group) return;
-  float top = -INFINITY, sum = 0.f, acc = 0.f;
-#pragma unroll 4
-  for (int x = rec.x; x <= c; ++x) {
-    const float* part = p.parts + (size_t)(2 * x + (x == rec.x ? 1 : 0)) * C::kPartFloats;
-    const float a = part[row * D + ch], m = part[C::kRows * D + row], l = part[C::kRows * (D + 1) + row];
-    const float m_new = fmaxf(top, m);
-    const float f = m_new == -INFINITY ? 1.f : ex2(top - m_new), f1 = m_new == -INFINITY ? 1.f : ex2(m - m_new);
-    acc = acc * f + a * f1;
-    sum = sum * f + l * f1;
-    top = m_new;
+  const bool on = full < r.queries * p.group;
+  auto part_of = [&](int x) { return p.parts + (size_t)(2 * x + (x == rec.x ? 1 : 0)) * C::kPartFloats; };
+  float top = -INFINITY, sum = 0.f, acc[kCh];
+#pragma unroll
+  for (int i = 0; i < kCh; ++i) acc[i] = 0.f;
+  if (on) {
+    for (int x = rec.x + lane; x <= c; x += 32) top = fmaxf(top, part_of(x)[C::kRows * D + row]);
+#pragma unroll
+    for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(kAll, top, o));
+#pragma unroll 8
+    for (int x = rec.x + share; x <= c; x += kShare) {
+      const float* part = part_of(x);
+      const float m = part[C::kRows * D + row], l = part[C::kRows * (D + 1) + row];
+      const float f = m == -INFINITY ? (top == -INFINITY ? 1.f : 0.f) : ex2(m - top);
+      float a[kCh];
+      if constexpr (kCh == 4) *reinterpret_cast<float4*>(a) = *reinterpret_cast<const float4*>(part + row * D + lane * 4);
+      else *reinterpret_cast<float2*>(a) = *reinterpret_cast<const float2*>(part + row * D + lane * 2);
+#pragma unroll
+      for (int i = 0; i < kCh; ++i) acc[i] += a[i] * f;
+      sum += l * f;
+    }
   }
+  if constexpr (kShare > 1) {
+#pragma unroll
+    for (int i = 0; i < kCh; ++i) joined[warp][lane * kCh + i] = acc[i];
+    if (lane == 0) joined[warp][D] = sum;
+    __syncthreads();
+    if (share > 0) return;
+#pragma unroll
+    for (int y = 1; y < kShare; ++y) {
+      sum += joined[y * C::kRows + row][D];
+#pragma unroll
+      for (int i = 0; i < kCh; ++i) acc[i] += joined[y * C::kRows + row][lane * kCh + i];
+    }
+  }
+  if (!on) return;
   const int qi = full / p.group, hq = rec.z * p.group + full - qi * p.group;
-  T* dst = (T*)p.out + (r.first + qi) * p.o_s[0] + hq * p.o_s[1];
-  dst[ch] = T(sum == 0.f ? 0.f : acc / sum * p.v_scale);
-  if (p.lse && ch == 0)
-    p.lse[(size_t)(r.first + qi) * p.Hq + hq] = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(sum) - kWeightShift) * kLn2;
+  T* dst = (T*)p.out + (r.first + qi) * p.o_s[0] + hq * p.o_s[1] + lane * kCh;
+  uint32_t w[kCh / 2];
+#pragma unroll
+  for (int i = 0; i < kCh / 2; ++i)
+    w[i] = sum == 0.f ? 0u : Two<T>::round(acc[2 * i] / sum * p.v_scale, acc[2 * i + 1] / sum * p.v_scale);
+  if constexpr (kCh == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+  else *reinterpret_cast<uint32_t*>(dst) = w[0];
+  if (p.lse && lane == 0)
+    p.lse[(size_t)(r.first + qi) * p.Hq + hq] = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(sum) - kShift) * kLn2;
 }
 
 constexpr int kBlocksPerSm = 4, kMostBlocks = 4 * 160;
@@ -513,7 +571,7 @@ cudaError_t run(const AttnParams& p, int sms, cudaStream_t stream, int* n) {
   cudaError_t e = launch_after(cache_attention_kernel<T, D, NB>, dim3(grid), kThreads, C::kSmem, C::kSmem, 0, stream, p);
   if (e == cudaSuccess) {
     ++*n;
-    e = launch_after(cache_combine_kernel<T, D, NB>, dim3(grid, C::kRows / kCombineRows), D * kCombineRows, 0, 0, 0, stream, p);
+    e = launch_after(cache_combine_kernel<T, D, NB>, dim3(grid), 32 * kJoinWarps, 0, 0, 0, stream, p);
     if (e == cudaSuccess) ++*n;
   }
   return e;
@@ -576,6 +634,8 @@ sol_status_t sol_attn_cache_attention(const sol_attn_cache_args* a) {
   p.sl2 = std::ldexp(scale * 1.4426950408889634f, a->cache.k_exp);
   p.v_scale = std::ldexp(1.0f, a->cache.v_exp);
   char* ws = static_cast<char*>(a->workspace);
+  p.wait_limit = fwd::g_wait_limit;
+  p.withhold = fwd::g_withhold_tile;
   p.status = reinterpret_cast<int32_t*>(ws);
   p.records = reinterpret_cast<int4*>(ws + cache::kRecordsAt);
   p.parts = reinterpret_cast<float*>(ws + cache::kRecordsAt + cache::kMostBlocks * sizeof(int4));

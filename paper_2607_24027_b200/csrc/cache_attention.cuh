@@ -18,6 +18,8 @@ struct AttnParams {
   float sl2;                                     // logit scale * log2(e) * 2^k_exp
   float v_scale;                                 // 2^v_exp
   int32_t* status;
+  long long wait_limit;                          // SM clocks after which a bounded wait gives up
+  int withhold;                                  // test hook: >= 0: the arrival for this step of each block is left out
   int4* records;                                 // per block: what it leaves to be combined
   float* parts;                                  // two partial results per block
 };

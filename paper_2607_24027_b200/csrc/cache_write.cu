@@ -130,10 +130,12 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const WriteParams 
     s8 = unit[U::key_scale(i, at.group)];
   }
   const float s = __low2float(cache::scales2(s8)) * cache::power2(at.is_value ? p.v_exp : p.k_exp);
-  uint32_t w[8];
+  uint32_t lo[4], hi[4], w[8];
+  cache::codes8((uint32_t)codes, lo);
+  cache::codes8((uint32_t)(codes >> 32), hi);
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const float2 f = __half22float2(cache::codes2((uint32_t)(codes >> (8 * j)) & 0xffu));
+    const float2 f = __half22float2(cache::half2_of(j < 4 ? lo[j % 4] : hi[j % 4]));
     w[j] = Two<T>::round(f.x * s, f.y * s);
   }
   dst += at.is_value ? at.token * p.v_s[0] + at.head * p.v_s[1] : at.token * p.k_s[0] + at.head * p.k_s[1];

@@ -114,7 +114,8 @@ def attention(q, cu, kv_lens, table, k, v, page_size, causal, scale, k_all_pages
     logit, d products of exact operands summed in fp32 with an error of 2^-23 of the partial sums at each step, the scaling
     (2^-23) and the subtraction of the maximum (2^-24 of its result, at most 2 largest logits).  Numerator and denominator both
     have the logits' error.  The sums over n keys in fp32: 2^-23 for each of the tree's n / 16 + 64 steps of its magnitude sum p |v|.
-    Weights below 2^-29 of the largest have an error of 2^-40 of it each."""
+    Weights are held as 2^11 times their ratio to an earlier maximum, which is no larger than the row's: fp16's subnormal numbers, below
+    2^-14, are 2^-24 apart, so small weights are off by 2^-25 / 2^11 = 2^-36 of the largest each."""
     T, H, d = q.shape
     Hk = k.shape[1]
     out, lse = torch.zeros(T, H, d, dtype=torch.float64), torch.full((T, H), -math.inf, dtype=torch.float64)
@@ -149,6 +150,6 @@ def attention(q, cu, kv_lens, table, k, v, page_size, causal, scale, k_all_pages
             wn = (w / torch.where(some, total, 1.0)[:, None]).nan_to_num(0)
             mass = wn @ vz.abs().nan_to_num(0)
             tol[lo:hi, h] = mass * (2.0 ** -11 + 2.0 ** -20 + 2 * logit[:, None] + (n / 16 + 64) * 2.0 ** -23) + \
-                n * 2.0 ** -40 * (vz.abs().nan_to_num(0).max() if n else 0)
+                n * 2.0 ** -36 * (vz.abs().nan_to_num(0).max() if n else 0)
             tol_lse[lo:hi, h] = 2 * logit + (n / 16 + 80) * 2.0 ** -23 + 2.0 ** -22 * lse[lo:hi, h].abs().nan_to_num(0, 0, 0)
     return out, lse, tol, tol_lse, touched
