@@ -28,6 +28,8 @@ constexpr unsigned kAll = 0xffffffffu;
 // Weights are 2^(x - m + kShift) with x the logit times log2(e) and m a maximum of earlier keys, which is replaced once a weight would
 // pass 2^kMost: fp16 holds them to 2^-12 down to 2^-25 of the largest, and is off by 2^-36 of it at most below.
 constexpr float kShift = 11.f, kMost = 15.f;
+constexpr int kBlocksPerSm = 4, kMostBlocks = 4 * 160;
+constexpr size_t kRecordsAt = 1024;              // in the workspace, behind the status word
 constexpr float kLn2 = 0.6931471805599453f;
 
 template <int D, int NB>
@@ -56,24 +58,12 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {     // an 8 x 8 mat
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
   return r;
 }
-// Sum over the block's threads.
-__device__ long long block_sum(long long x, long long* warps) {
-  for (int o = 16; o; o /= 2) x += __shfl_xor_sync(kAll, x, o);
-  __syncthreads();
-  if (threadIdx.x % 32 == 0) warps[threadIdx.x / 32] = x;
-  __syncthreads();
-  long long s = 0;
-  for (int w = 0; w < kWarps; ++w) s += warps[w];
-  return s;
-}
-
 struct Shared {
   uint64_t full[kStages], empty[kStages];        // a step has landed; all warps are done with it
   int abort_flag;
   int missing;                                   // a page of this piece is not there
-  long long warps[kWarps];
-  long long base;                                // first step of request `start`
-  int start;
+  long long sums[kWarps];
+  Start start;
 };
 
 template <class T, int D, int NB>
@@ -94,48 +84,17 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
   kernel_wait();
   kernel_release();                              // (the joining kernel's blocks find room only as this one's leave)
 
-  // ---- this block's share
-  long long mine = 0;
-  for (int b = tid; b < p.requests; b += kThreads) {
-    const Request r = request_at(p, b);
-    mine += Work(r, p.group, C::kRows, kStep).total(p.Hk);
-  }
-  const long long work = block_sum(mine, sh.warps);
-  const long long blocks = min((long long)gridDim.x, work);
-  if ((long long)blockIdx.x >= blocks) {
-    if (tid == 0) p.records[blockIdx.x] = make_int4(-1, 0, 0, 0);
+  const Shares shares = find_share<kThreads>(p, C::kRows, kStep, blockIdx.x, sh.sums, &sh.start);
+  if ((long long)blockIdx.x >= shares.blocks) {
+    if (tid == 0) p.records[blockIdx.x] = Record{-1, 0, 0, 0, 0, 0, 0, 0};
     return;
   }
-  long long w = share_begin(work, blocks, blockIdx.x);
-  const long long w_end = share_begin(work, blocks, blockIdx.x + 1);
-  {
-    long long base = 0;
-    for (int b0 = 0; b0 < p.requests; b0 += kThreads) {
-      const int b = b0 + tid;
-      long long n = 0;
-      if (b < p.requests) n = Work(request_at(p, b), p.group, C::kRows, kStep).total(p.Hk);
-      long long x = n;
-      for (int o = 1; o < 32; o *= 2) {
-        const long long y = __shfl_up_sync(kAll, x, o);
-        if (lane >= o) x += y;
-      }
-      __syncthreads();
-      if (lane == 31) sh.warps[warp] = x;
-      __syncthreads();
-      long long before = 0, all = 0;
-      for (int i = 0; i < kWarps; ++i) { if (i < warp) before += sh.warps[i]; all += sh.warps[i]; }
-      const long long lo = base + before + x - n;
-      if (n > 0 && lo <= w && w < lo + n) { sh.start = b; sh.base = lo; }
-      base += all;
-      if (w < base) break;                       // (the whole block)
-    }
-    __syncthreads();
-  }
-  int b = sh.start;
-  long long base = sh.base;
-  Request r = request_at(p, b);
-  Work wk(r, p.group, C::kRows, kStep);
-  int4 record = make_int4(-1, 0, 0, 0);
+  long long w = shares.begin(blockIdx.x), base = sh.start.base;
+  const long long w_end = shares.begin(blockIdx.x + 1);
+  int b = sh.start.index;
+  Request r = sh.start.request;
+  Work wk(p, r, C::kRows, kStep);
+  Record record{-1, 0, 0, 0, 0, 0, 0, 0};
   bool first_piece = true, ok = true;
   uint32_t fetches = 0;                          // steps of earlier pieces
 
@@ -144,13 +103,52 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
       base += wk.total(p.Hk);
       ++b;
       r = request_at(p, b);
-      wk = Work(r, p.group, C::kRows, kStep);
+      wk = Work(p, r, C::kRows, kStep);
     }
-    const long long item = (w - base) / wk.steps;
-    const int head = (int)(item / wk.tiles), tile = (int)(item - (long long)head * wk.tiles);
+    const long long item = quotient(w - base, wk.steps);
+    const int head = (int)quotient(item, wk.tiles), tile = (int)(item - (long long)head * wk.tiles);
     const long long item_begin = base + item * wk.steps, item_end = item_begin + wk.steps;
     const int s_begin = (int)(w - item_begin), s_end = (int)(min(w_end, item_end) - item_begin);
     const int rows = r.queries * p.group;
+
+    // ---- how the steps come in
+    const uint32_t page_bytes = (uint32_t)p.Hk * ((uint32_t)U::kBytes << (p.page_shift - 4));
+    const unsigned char* head_data = p.data + (size_t)head * ((size_t)U::kBytes << (p.page_shift - 4));
+    const int32_t* table = p.tables + b * p.table_stride;
+    const int units = (r.keys + kUnit - 1) / kUnit;
+    auto unit_of = [&](int step, int i) { return step * (kStep / kUnit) + warp * 2 + i; };
+    auto page_at = [&](int unit) {               // -1: there is none
+      const int page = unit < units ? table[unit >> (p.page_shift - 4)] : -1;
+      return page < p.pages ? page : -1;
+    };
+    // A step is fetched by one warp, the warps in turn: by one copy, or one for each page if pages are smaller, a lane each.
+    const int per = min(kStep / kUnit, 1 << (p.page_shift - 4));               // units of a copy
+    auto fetch = [&](int step) {
+      if (step >= s_end) return;
+      const uint32_t n = fetches + (uint32_t)(step - s_begin), s = n % kStages;
+      if (n >= kStages && !__all_sync(kAll, mbar_wait(&sh.empty[s], (n / kStages - 1) & 1, &sh.abort_flag, p.wait_limit))) {
+        ok = false;
+        return;
+      }
+      uint64_t* bar = &sh.full[s];
+      const int u = step * (kStep / kUnit) + lane * per;
+      if (lane * per < kStep / kUnit && u < units) {
+        const int page = table[u >> (p.page_shift - 4)];
+        if (page >= 0 && page < p.pages) {
+          const uint32_t in_page = (uint32_t)u & ((1u << (p.page_shift - 4)) - 1);
+          const uint32_t bytes = (uint32_t)min(per, units - u) * U::kBytes;
+          mbar_expect_tx(bar, bytes);
+          bulk_load_1d(smem + s * C::kStageBytes + lane * per * U::kBytes, head_data + (size_t)(uint32_t)page * page_bytes + in_page * U::kBytes,
+                       bytes, bar);
+        } else {
+          sh.missing = 1;
+        }
+      }
+      __syncwarp();
+      if (lane == 0 && (int)n != p.withhold) mbar_arrive(bar);                 // (a test withholds it)
+    };
+
+    if (warp < kStages - 1) fetch(s_begin + warp);
 
     // ---- the rows' queries as the products' 8-sided operand, scaled by a power of two per row so that fp16 holds them
     uint32_t qf[NB][kSteps16][2];
@@ -217,43 +215,6 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
 #pragma unroll
       for (int j = 0; j < 2; ++j) { nm[nb][j] = 0.f; l[nb][j] = 0.f; seen[nb][j] = false; }
     }
-
-    // ---- the steps
-    const uint32_t page_bytes = (uint32_t)p.Hk * ((uint32_t)U::kBytes << (p.page_shift - 4));
-    const unsigned char* head_data = p.data + (size_t)head * ((size_t)U::kBytes << (p.page_shift - 4));
-    const int32_t* table = p.tables + b * p.table_stride;
-    const int units = (r.keys + kUnit - 1) / kUnit;
-    auto unit_of = [&](int step, int i) { return step * (kStep / kUnit) + warp * 2 + i; };
-    auto page_at = [&](int unit) {               // -1: there is none
-      const int page = unit < units ? table[unit >> (p.page_shift - 4)] : -1;
-      return page < p.pages ? page : -1;
-    };
-    // A step is fetched by one warp, the warps in turn: by one copy, or one for each page if pages are smaller, a lane each.
-    const int per = min(kStep / kUnit, 1 << (p.page_shift - 4));               // units of a copy
-    auto fetch = [&](int step) {
-      if (step >= s_end) return;
-      const uint32_t n = fetches + (uint32_t)(step - s_begin), s = n % kStages;
-      if (n >= kStages && !__all_sync(kAll, mbar_wait(&sh.empty[s], (n / kStages - 1) & 1, &sh.abort_flag, p.wait_limit))) {
-        ok = false;
-        return;
-      }
-      uint64_t* bar = &sh.full[s];
-      const int u = step * (kStep / kUnit) + lane * per;
-      if (lane * per < kStep / kUnit && u < units) {
-        const int page = table[u >> (p.page_shift - 4)];
-        if (page >= 0 && page < p.pages) {
-          const uint32_t in_page = (uint32_t)u & ((1u << (p.page_shift - 4)) - 1);
-          const uint32_t bytes = (uint32_t)min(per, units - u) * U::kBytes;
-          mbar_expect_tx(bar, bytes);
-          bulk_load_1d(smem + s * C::kStageBytes + lane * per * U::kBytes, head_data + (size_t)(uint32_t)page * page_bytes + in_page * U::kBytes,
-                       bytes, bar);
-        } else {
-          sh.missing = 1;
-        }
-      }
-      __syncwarp();
-      if (lane == 0 && (int)n != p.withhold) mbar_arrive(bar);                 // (a test withholds it)
-    };
 
     // one step of 2 x 16 keys, all of which all rows see if `Whole`
     auto work_on = [&](int step, const unsigned char* stage, auto whole) {
@@ -404,7 +365,6 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
       }
     };
 
-    if (warp < kStages - 1) fetch(s_begin + warp);
     uint32_t n = fetches;
     for (int step = s_begin; ok && step < s_end; ++step, ++n) {
       const uint32_t s = n % kStages;
@@ -427,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
       int never = 0;
       if (!ok)
         for (uint32_t x = n; x < n + kStages; ++x) mbar_wait(&sh.full[x % kStages], (x / kStages) & 1, &never, p.wait_limit);
-      if (tid == 0) p.records[blockIdx.x] = make_int4(-1, 0, 0, 0);
+      if (tid == 0) p.records[blockIdx.x] = Record{-1, 0, 0, 0, 0, 0, 0, 0};
       return;
     }
     fetches += (uint32_t)(s_end - s_begin);
@@ -486,7 +446,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
       }
     }
     if (!begins && ends)                         // the last piece of a cut item: this block's record has it combined
-      record = make_int4((int)owner_of(work, blocks, item_begin), b, head, tile);
+      record = Record{(int)shares.owner(item_begin), head, tile, r.queries, r.first, 0, 0, 0};
     if (tid == 0) sh.missing = 0;
     fence_proxy_async_smem();                    // the next copies go where the warps' results were
     __syncthreads();
@@ -496,72 +456,120 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
   if (tid == 0) p.records[blockIdx.x] = record;
 }
 
-// Joins the pieces of an item that several blocks had: block c of the first kernel had the last piece, blocks records[c].x ... c - 1
-// the others.  The block that had the first piece left it in its second place, the rest in their first.  A row is added up by
-// kJoinWarps / rows warps, four channels (two, d = 64) to a lane.
-constexpr int kJoinWarps = 16;
+// Joins the pieces of the items that several blocks had: block c of the first kernel had the last piece, blocks from record.from to c
+// - 1 the others.  The block that had the first piece left it in its second place, the rest in their first.  A row is added up
+// by `share` warps, four channels (two, d = 64) to a lane: with many items to join, which then have few pieces, by one, else by 16.
+// What bounds this kernel is the way to memory and back, so there are two on its longest path: the records, and up to 8 pieces at once.
+constexpr int kJoinWarps = 16, kManyRecords = 64, kAtOnce = 8;
 template <class T, int D, int NB>
-__global__ void __launch_bounds__(32 * kJoinWarps) cache_combine_kernel(const AttnParams p) {
+__global__ void __launch_bounds__(32 * kJoinWarps) cache_combine_kernel(const AttnParams p, int records) {
   using C = Cfg<D, NB>;
-  constexpr int kShare = kJoinWarps / C::kRows, kCh = D / 32;
+  constexpr int kCh = D / 32;
   __shared__ float joined[kJoinWarps][D + 2];
+  __shared__ int counts[kJoinWarps];
+  __shared__ Record list[kMostBlocks];
+  __shared__ short last_of[kMostBlocks];
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   kernel_wait();
-  const int c = blockIdx.x;
-  const int4 rec = p.records[c];
-  if (rec.x < 0) return;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, row = warp % C::kRows, share = warp / C::kRows;
-  const Request r = request_at(p, rec.y);
-  const int full = rec.w * C::kRows + row;
-  const bool on = full < r.queries * p.group;
-  auto part_of = [&](int x) { return p.parts + (size_t)(2 * x + (x == rec.x ? 1 : 0)) * C::kPartFloats; };
-  float top = -INFINITY, sum = 0.f, acc[kCh];
-#pragma unroll
-  for (int i = 0; i < kCh; ++i) acc[i] = 0.f;
-  if (on) {
-    for (int x = rec.x + lane; x <= c; x += 32) top = fmaxf(top, part_of(x)[C::kRows * D + row]);
-#pragma unroll
-    for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(kAll, top, o));
-#pragma unroll 8
-    for (int x = rec.x + share; x <= c; x += kShare) {
-      const float* part = part_of(x);
-      const float m = part[C::kRows * D + row], l = part[C::kRows * (D + 1) + row];
-      const float f = m == -INFINITY ? (top == -INFINITY ? 1.f : 0.f) : ex2(m - top);
-      float a[kCh];
-      if constexpr (kCh == 4) *reinterpret_cast<float4*>(a) = *reinterpret_cast<const float4*>(part + row * D + lane * 4);
-      else *reinterpret_cast<float2*>(a) = *reinterpret_cast<const float2*>(part + row * D + lane * 2);
-#pragma unroll
-      for (int i = 0; i < kCh; ++i) acc[i] += a[i] * f;
-      sum += l * f;
-    }
-  }
-  if constexpr (kShare > 1) {
-#pragma unroll
-    for (int i = 0; i < kCh; ++i) joined[warp][lane * kCh + i] = acc[i];
-    if (lane == 0) joined[warp][D] = sum;
+  // the records, packed
+  int n = 0;
+  for (int c0 = 0; c0 < records; c0 += 32 * kJoinWarps) {
+    const int c = c0 + tid;
+    Record rec{-1, 0, 0, 0, 0, 0, 0, 0};
+    if (c < records) rec = p.records[c];
+    const unsigned some = __ballot_sync(kAll, rec.from >= 0);
+    if (lane == 0) counts[warp] = __popc(some);
     __syncthreads();
-    if (share > 0) return;
-#pragma unroll
-    for (int y = 1; y < kShare; ++y) {
-      sum += joined[y * C::kRows + row][D];
-#pragma unroll
-      for (int i = 0; i < kCh; ++i) acc[i] += joined[y * C::kRows + row][lane * kCh + i];
+    int at = n;
+    for (int x = 0; x < kJoinWarps; ++x) {
+      if (x == warp && rec.from >= 0) {
+        const int k = at + __popc(some & ((1u << lane) - 1));
+        list[k] = rec;
+        last_of[k] = (short)c;
+      }
+      at += counts[x];
     }
+    n = at;
+    __syncthreads();
   }
-  if (!on) return;
-  const int qi = full / p.group, hq = rec.z * p.group + full - qi * p.group;
-  T* dst = (T*)p.out + (r.first + qi) * p.o_s[0] + hq * p.o_s[1] + lane * kCh;
-  uint32_t w[kCh / 2];
+  const int share = n >= kManyRecords ? 1 : kJoinWarps, rows_at_once = kJoinWarps / share;
+  const int tasks = n * C::kRows;
+  for (int t0 = blockIdx.x * rows_at_once; t0 < tasks; t0 += gridDim.x * rows_at_once) {
+    const int task = t0 + warp / share, part0 = warp % share;
+    const bool is = task < tasks;
+    const Record rec = list[is ? task / C::kRows : 0];
+    const int last = last_of[is ? task / C::kRows : 0], row = task % C::kRows;
+    const int full = rec.tile * C::kRows + row;
+    const bool on = is && full < rec.queries * p.group;
+    float top = -INFINITY, sum = 0.f, acc[kCh];
 #pragma unroll
-  for (int i = 0; i < kCh / 2; ++i)
-    w[i] = sum == 0.f ? 0u : Two<T>::round(acc[2 * i] / sum * p.v_scale, acc[2 * i + 1] / sum * p.v_scale);
-  if constexpr (kCh == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
-  else *reinterpret_cast<uint32_t*>(dst) = w[0];
-  if (p.lse && lane == 0)
-    p.lse[(size_t)(r.first + qi) * p.Hq + hq] = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(sum) - kShift) * kLn2;
+    for (int i = 0; i < kCh; ++i) acc[i] = 0.f;
+    for (int x0 = rec.from + part0; on && x0 <= last; x0 += share * kAtOnce) {
+      float m[kAtOnce], l[kAtOnce], a[kAtOnce][kCh], most = top;
+#pragma unroll
+      for (int y = 0; y < kAtOnce; ++y) {
+        const int x = x0 + y * share;
+        const float* part = p.parts + (size_t)(2 * x + (x == rec.from ? 1 : 0)) * C::kPartFloats;
+        m[y] = -INFINITY; l[y] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kCh; ++i) a[y][i] = 0.f;
+        if (x <= last) {
+          m[y] = part[C::kRows * D + row];
+          l[y] = part[C::kRows * (D + 1) + row];
+          if constexpr (kCh == 4) *reinterpret_cast<float4*>(a[y]) = *reinterpret_cast<const float4*>(part + row * D + lane * 4);
+          else *reinterpret_cast<float2*>(a[y]) = *reinterpret_cast<const float2*>(part + row * D + lane * 2);
+        }
+      }
+#pragma unroll
+      for (int y = 0; y < kAtOnce; ++y) most = fmaxf(most, m[y]);
+      const float f0 = top == -INFINITY ? 1.f : ex2(top - most);               // (then acc and sum are 0 or NaN)
+#pragma unroll
+      for (int i = 0; i < kCh; ++i) acc[i] *= f0;
+      sum *= f0;
+      top = most;
+#pragma unroll
+      for (int y = 0; y < kAtOnce; ++y) {
+        const float f = m[y] == -INFINITY ? 1.f : ex2(m[y] - top);             // (a piece without a maximum holds 0 or NaN)
+#pragma unroll
+        for (int i = 0; i < kCh; ++i) acc[i] += a[y][i] * f;
+        sum += l[y] * f;
+      }
+    }
+    if (share > 1) {
+      __syncthreads();                           // (the last round's readers)
+#pragma unroll
+      for (int i = 0; i < kCh; ++i) joined[warp][lane * kCh + i] = acc[i];
+      if (lane == 0) { joined[warp][D] = sum; joined[warp][D + 1] = top; }
+      __syncthreads();
+      if (part0 > 0) continue;
+      float most = lane < kJoinWarps ? joined[lane][D + 1] : -INFINITY;
+#pragma unroll
+      for (int o = 16; o; o /= 2) most = fmaxf(most, __shfl_xor_sync(kAll, most, o));
+      top = most;
+      sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < kCh; ++i) acc[i] = 0.f;
+#pragma unroll
+      for (int y = 0; y < kJoinWarps; ++y) {
+        const float m = joined[y][D + 1], f = m == -INFINITY ? 1.f : ex2(m - top);
+        sum += joined[y][D] * f;
+#pragma unroll
+        for (int i = 0; i < kCh; ++i) acc[i] += joined[y][lane * kCh + i] * f;
+      }
+    }
+    if (!on) continue;
+    const int qi = full / p.group, hq = rec.head * p.group + full - qi * p.group;
+    T* dst = (T*)p.out + (rec.first + qi) * p.o_s[0] + hq * p.o_s[1] + lane * kCh;
+    uint32_t w[kCh / 2];
+#pragma unroll
+    for (int i = 0; i < kCh / 2; ++i)
+      w[i] = sum == 0.f ? 0u : Two<T>::round(acc[2 * i] / sum * p.v_scale, acc[2 * i + 1] / sum * p.v_scale);
+    if constexpr (kCh == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint32_t*>(dst) = w[0];
+    if (p.lse && lane == 0)
+      p.lse[(size_t)(rec.first + qi) * p.Hq + hq] = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(sum) - kShift) * kLn2;
+  }
 }
-
-constexpr int kBlocksPerSm = 4, kMostBlocks = 4 * 160;
-constexpr size_t kRecordsAt = 1024;
 
 template <class T, int D, int NB>
 cudaError_t run(const AttnParams& p, int sms, cudaStream_t stream, int* n) {
@@ -571,7 +579,7 @@ cudaError_t run(const AttnParams& p, int sms, cudaStream_t stream, int* n) {
   cudaError_t e = launch_after(cache_attention_kernel<T, D, NB>, dim3(grid), kThreads, C::kSmem, C::kSmem, 0, stream, p);
   if (e == cudaSuccess) {
     ++*n;
-    e = launch_after(cache_combine_kernel<T, D, NB>, dim3(grid), 32 * kJoinWarps, 0, 0, 0, stream, p);
+    e = launch_after(cache_combine_kernel<T, D, NB>, dim3(2 * sms), 32 * kJoinWarps, 0, 0, 0, stream, p, grid);
     if (e == cudaSuccess) ++*n;
   }
   return e;
@@ -579,7 +587,7 @@ cudaError_t run(const AttnParams& p, int sms, cudaStream_t stream, int* n) {
 
 size_t workspace_bytes(int rows, int d) {
   const size_t r = rows <= 8 ? 8 : 16;
-  return align_up(kRecordsAt + kMostBlocks * sizeof(int4) + 2 * kMostBlocks * r * (d + 2) * sizeof(float), 1024);
+  return align_up(kRecordsAt + kMostBlocks * sizeof(cache::Record) + 2 * kMostBlocks * r * (d + 2) * sizeof(float), 1024);
 }
 
 sol_status_t check_attention(const sol_attn_cache_args* a) {
@@ -634,11 +642,12 @@ sol_status_t sol_attn_cache_attention(const sol_attn_cache_args* a) {
   p.sl2 = std::ldexp(scale * 1.4426950408889634f, a->cache.k_exp);
   p.v_scale = std::ldexp(1.0f, a->cache.v_exp);
   char* ws = static_cast<char*>(a->workspace);
+  p.rows_from = 0; p.rows_to = 0x7fffffffffffLL;
   p.wait_limit = fwd::g_wait_limit;
   p.withhold = fwd::g_withhold_tile;
   p.status = reinterpret_cast<int32_t*>(ws);
-  p.records = reinterpret_cast<int4*>(ws + cache::kRecordsAt);
-  p.parts = reinterpret_cast<float*>(ws + cache::kRecordsAt + cache::kMostBlocks * sizeof(int4));
+  p.records = reinterpret_cast<cache::Record*>(ws + cache::kRecordsAt);
+  p.parts = reinterpret_cast<float*>(ws + cache::kRecordsAt + cache::kMostBlocks * sizeof(cache::Record));
   const cudaStream_t stream = static_cast<cudaStream_t>(a->stream);
   int n = 0;
   auto typed = [&](auto zero) {
