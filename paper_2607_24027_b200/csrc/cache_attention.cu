@@ -25,12 +25,10 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kWarpKeys = 32, kStep = kWarps * kWarpKeys;
 constexpr int kStages = 3;
 constexpr unsigned kAll = 0xffffffffu;
-// Weights are 2^(x - m + kShift) with x the logit times log2(e) and m a maximum of earlier keys, which is replaced once a weight would
-// pass 2^kMost: fp16 holds them to 2^-12 down to 2^-25 of the largest, and is off by 2^-36 of it at most below.
-constexpr float kShift = 11.f, kMost = 15.f;
-constexpr int kBlocksPerSm = 4, kMostBlocks = 4 * 160;
-constexpr size_t kRecordsAt = 1024;              // in the workspace, behind the status word
-constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kBlocksPerSm = 4;
+constexpr long long kAnyRows = 1LL << 40;
+// Requests of up to so many rows (queries times the query heads of a key / value head) are this kernel's.
+constexpr long long kFewRows = 64;
 
 template <int D, int NB>
 struct Cfg {
@@ -67,7 +65,7 @@ struct Shared {
 };
 
 template <class T, int D, int NB>
-__global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_kernel(const AttnParams p) {
+__global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_kernel(const __grid_constant__ AttnParams p) {
   using C = Cfg<D, NB>;
   using U = Unit<D>;
   constexpr int kSteps16 = D / 16;               // products of 16 channels; also 16-channel tiles of the values
@@ -84,37 +82,27 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
   kernel_wait();
   kernel_release();                              // (the joining kernel's blocks find room only as this one's leave)
 
-  const Shares shares = find_share<kThreads>(p, C::kRows, kStep, blockIdx.x, sh.sums, &sh.start);
+  using Tiling = Tiles<C::kRows, kStep>;
+  const Shares shares = find_share<kThreads, Tiling>(p, blockIdx.x, sh.sums, &sh.start);
   if ((long long)blockIdx.x >= shares.blocks) {
     if (tid == 0) p.records[blockIdx.x] = Record{-1, 0, 0, 0, 0, 0, 0, 0};
     return;
   }
-  long long w = shares.begin(blockIdx.x), base = sh.start.base;
-  const long long w_end = shares.begin(blockIdx.x + 1);
-  int b = sh.start.index;
-  Request r = sh.start.request;
-  Work wk(p, r, C::kRows, kStep);
+  Pieces<Tiling> at;
+  at.start(p, sh.start, shares.begin(blockIdx.x), shares.begin(blockIdx.x + 1));
   Record record{-1, 0, 0, 0, 0, 0, 0, 0};
-  bool first_piece = true, ok = true;
+  bool ok = true;
   uint32_t fetches = 0;                          // steps of earlier pieces
 
-  while (w < w_end) {
-    while (w >= base + wk.total(p.Hk)) {         // next request with work
-      base += wk.total(p.Hk);
-      ++b;
-      r = request_at(p, b);
-      wk = Work(p, r, C::kRows, kStep);
-    }
-    const long long item = quotient(w - base, wk.steps);
-    const int head = (int)quotient(item, wk.tiles), tile = (int)(item - (long long)head * wk.tiles);
-    const long long item_begin = base + item * wk.steps, item_end = item_begin + wk.steps;
-    const int s_begin = (int)(w - item_begin), s_end = (int)(min(w_end, item_end) - item_begin);
+  while (at.next(p)) {
+    const Request r = at.r;
+    const int head = at.head, tile = at.tile, s_begin = at.s_begin, s_end = at.s_end;
     const int rows = r.queries * p.group;
 
     // ---- how the steps come in
     const uint32_t page_bytes = (uint32_t)p.Hk * ((uint32_t)U::kBytes << (p.page_shift - 4));
     const unsigned char* head_data = p.data + (size_t)head * ((size_t)U::kBytes << (p.page_shift - 4));
-    const int32_t* table = p.tables + b * p.table_stride;
+    const int32_t* table = p.tables + at.b * p.table_stride;
     const int units = (r.keys + kUnit - 1) / kUnit;
     auto unit_of = [&](int step, int i) { return step * (kStep / kUnit) + warp * 2 + i; };
     auto page_at = [&](int unit) {               // -1: there is none
@@ -419,8 +407,8 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
           *reinterpret_cast<float2*>(dst + 2 * s) = make_float2(o[nb][s][j] * f, o[nb][s][2 + j] * f);
       }
     __syncthreads();
-    const bool begins = s_begin == 0, ends = s_end == wk.steps;
-    float* part = p.parts + (size_t)(2 * blockIdx.x + (first_piece && !begins ? 0 : 1)) * C::kPartFloats;
+    const bool begins = at.begins(), ends = at.ends();
+    float* part = p.parts + (size_t)(2 * blockIdx.x + (begins ? 1 : 0)) * C::kPartFloats;
     for (int x = tid; x < C::kRows * D; x += kThreads) {
       const int row = x / D, ch = x - row * D;
       float top = -INFINITY, sum = 0.f, acc = 0.f;
@@ -446,39 +434,38 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
       }
     }
     if (!begins && ends)                         // the last piece of a cut item: this block's record has it combined
-      record = Record{(int)shares.owner(item_begin), head, tile, r.queries, r.first, 0, 0, 0};
+      record = Record{(int)shares.owner(at.item_begin), head, tile, r.queries, r.first, 0, 0, 0};
     if (tid == 0) sh.missing = 0;
     fence_proxy_async_smem();                    // the next copies go where the warps' results were
     __syncthreads();
-    first_piece = false;
-    w = item_begin + s_end;
   }
   if (tid == 0) p.records[blockIdx.x] = record;
 }
 
 // Joins the pieces of the items that several blocks had: block c of the first kernel had the last piece, blocks from record.from to c
 // - 1 the others.  The block that had the first piece left it in its second place, the rest in their first.  A row is added up
-// by `share` warps, four channels (two, d = 64) to a lane: with many items to join, which then have few pieces, by one, else by 16.
+// by as many warps as it takes for each to have kAtOnce pieces, up to 16, four channels (two, d = 64) to a lane.
 // What bounds this kernel is the way to memory and back, so there are two on its longest path: the records, and up to 8 pieces at once.
-constexpr int kJoinWarps = 16, kManyRecords = 64, kAtOnce = 8;
+constexpr int kJoinWarps = 16, kAtOnce = 8;
 template <class T, int D, int NB>
-__global__ void __launch_bounds__(32 * kJoinWarps) cache_combine_kernel(const AttnParams p, int records) {
+__global__ void __launch_bounds__(32 * kJoinWarps) cache_combine_kernel(const __grid_constant__ AttnParams p, int records) {
   using C = Cfg<D, NB>;
   constexpr int kCh = D / 32;
   __shared__ float joined[kJoinWarps][D + 2];
-  __shared__ int counts[kJoinWarps];
+  __shared__ int counts[kJoinWarps], spans[kJoinWarps];
   __shared__ Record list[kMostBlocks];
   __shared__ short last_of[kMostBlocks];
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   kernel_wait();
   // the records, packed
-  int n = 0;
+  int n = 0, most_pieces = 0;
   for (int c0 = 0; c0 < records; c0 += 32 * kJoinWarps) {
     const int c = c0 + tid;
     Record rec{-1, 0, 0, 0, 0, 0, 0, 0};
     if (c < records) rec = p.records[c];
     const unsigned some = __ballot_sync(kAll, rec.from >= 0);
-    if (lane == 0) counts[warp] = __popc(some);
+    const int span = __reduce_max_sync(kAll, rec.from >= 0 ? c - rec.from + 1 : 0);
+    if (lane == 0) { counts[warp] = __popc(some); spans[warp] = span; }
     __syncthreads();
     int at = n;
     for (int x = 0; x < kJoinWarps; ++x) {
@@ -488,11 +475,14 @@ __global__ void __launch_bounds__(32 * kJoinWarps) cache_combine_kernel(const At
         last_of[k] = (short)c;
       }
       at += counts[x];
+      most_pieces = max(most_pieces, spans[x]);
     }
     n = at;
     __syncthreads();
   }
-  const int share = n >= kManyRecords ? 1 : kJoinWarps, rows_at_once = kJoinWarps / share;
+  int share = 1;
+  while (share < kJoinWarps && share * kAtOnce < most_pieces) share *= 2;
+  const int rows_at_once = kJoinWarps / share;
   const int tasks = n * C::kRows;
   for (int t0 = blockIdx.x * rows_at_once; t0 < tasks; t0 += gridDim.x * rows_at_once) {
     const int task = t0 + warp / share, part0 = warp % share;
@@ -542,15 +532,14 @@ __global__ void __launch_bounds__(32 * kJoinWarps) cache_combine_kernel(const At
       if (lane == 0) { joined[warp][D] = sum; joined[warp][D + 1] = top; }
       __syncthreads();
       if (part0 > 0) continue;
-      float most = lane < kJoinWarps ? joined[lane][D + 1] : -INFINITY;
+      float most = lane < share ? joined[warp + lane][D + 1] : -INFINITY;
 #pragma unroll
       for (int o = 16; o; o /= 2) most = fmaxf(most, __shfl_xor_sync(kAll, most, o));
       top = most;
       sum = 0.f;
 #pragma unroll
       for (int i = 0; i < kCh; ++i) acc[i] = 0.f;
-#pragma unroll
-      for (int y = 0; y < kJoinWarps; ++y) {
+      for (int y = warp; y < warp + share; ++y) {
         const float m = joined[y][D + 1], f = m == -INFINITY ? 1.f : ex2(m - top);
         sum += joined[y][D] * f;
 #pragma unroll
@@ -572,22 +561,52 @@ __global__ void __launch_bounds__(32 * kJoinWarps) cache_combine_kernel(const At
 }
 
 template <class T, int D, int NB>
-cudaError_t run(const AttnParams& p, int sms, cudaStream_t stream, int* n) {
-  using C = Cfg<D, NB>;
-  int grid = (NB == 1 ? kBlocksPerSm : kBlocksPerSm - 1) * sms;
-  if (grid > kMostBlocks) grid = kMostBlocks;
-  cudaError_t e = launch_after(cache_attention_kernel<T, D, NB>, dim3(grid), kThreads, C::kSmem, C::kSmem, 0, stream, p);
-  if (e == cudaSuccess) {
-    ++*n;
-    e = launch_after(cache_combine_kernel<T, D, NB>, dim3(2 * sms), 32 * kJoinWarps, 0, 0, 0, stream, p, grid);
-    if (e == cudaSuccess) ++*n;
-  }
+cudaError_t join(const AttnParams& p, int grid, int sms, cudaStream_t stream, int* n) {
+  const cudaError_t e = launch_after(cache_combine_kernel<T, D, NB>, dim3(2 * sms), 32 * kJoinWarps, 0, 0, 0, stream, p, grid);
+  if (e == cudaSuccess) ++*n;
   return e;
 }
 
-size_t workspace_bytes(int rows, int d) {
-  const size_t r = rows <= 8 ? 8 : 16;
-  return align_up(kRecordsAt + kMostBlocks * sizeof(cache::Record) + 2 * kMostBlocks * r * (d + 2) * sizeof(float), 1024);
+template <class T, int D, int NB>
+cudaError_t run_few(AttnParams p, long long rows_to, int sms, cudaStream_t stream, int* n) {
+  using C = Cfg<D, NB>;
+  p.rows_from = 0;
+  p.rows_to = rows_to;
+  int grid = (NB == 1 ? kBlocksPerSm : kBlocksPerSm - 1) * sms;
+  if (grid > kMostBlocks) grid = kMostBlocks;
+  const cudaError_t e = launch_after(cache_attention_kernel<T, D, NB>, dim3(grid), kThreads, C::kSmem, C::kSmem, 0, stream, p);
+  if (e != cudaSuccess) return e;
+  ++*n;
+  return join<T, D, NB>(p, grid, sms, stream, n);
+}
+
+template <class T, int D>
+cudaError_t run_many(AttnParams p, long long rows_from, int type, int sms, cudaStream_t stream, int* n) {
+  p.rows_from = rows_from;
+  p.rows_to = kAnyRows;
+  int grid = 0;
+  const cudaError_t e = launch_chunk(p, D, type, sms, stream, &grid);
+  if (e != cudaSuccess) return e;
+  ++*n;
+  return join<T, D, kChunkRows / 8>(p, grid, sms, stream, n);
+}
+
+template <class T, int D>
+cudaError_t run(const AttnParams& p, int max_q, int type, int sms, cudaStream_t stream, int* n) {
+  const long long rows = (long long)max_q * p.group;
+  if (rows <= 8) return run_few<T, D, 1>(p, kAnyRows, sms, stream, n);
+  if (rows <= kFewRows) return run_few<T, D, 2>(p, kAnyRows, sms, stream, n);
+  if (p.requests > 1) {                          // there may be some of either kind
+    const cudaError_t e = run_few<T, D, 2>(p, kFewRows, sms, stream, n);
+    if (e != cudaSuccess) return e;
+  }
+  return run_many<T, D>(p, p.requests > 1 ? kFewRows + 1 : 0, type, sms, stream, n);
+}
+
+size_t workspace_bytes(long long rows, int d) {
+  const size_t few = kMostBlocks * sizeof(Record) + 2 * kMostBlocks * (rows <= 8 ? 8 : 16) * (d + 2) * sizeof(float);
+  const size_t many = rows <= kFewRows ? 0 : kMostBlocks * sizeof(Record) + 2 * kMostChunkBlocks * kChunkRows * (size_t)(d + 2) * sizeof(float);
+  return align_up(kRecordsAt + (few > many ? few : many), 1024);
 }
 
 sol_status_t check_attention(const sol_attn_cache_args* a) {
@@ -617,7 +636,7 @@ extern "C" {
 size_t sol_attn_cache_workspace_bytes(int max_q, int Hq, int Hk, int d) {
   if (max_q <= 0 || Hq <= 0 || Hk <= 0 || Hq > sol::cache::kMaxHeads || Hq % Hk || (d != 64 && d != 128)) return 0;
   const long long rows = (long long)max_q * (Hq / Hk);
-  return sol::cache::workspace_bytes(rows > 16 ? 16 : (int)rows, d);
+  return sol::cache::workspace_bytes(rows, d);
 }
 
 sol_status_t sol_attn_cache_attention(const sol_attn_cache_args* a) {
@@ -642,7 +661,6 @@ sol_status_t sol_attn_cache_attention(const sol_attn_cache_args* a) {
   p.sl2 = std::ldexp(scale * 1.4426950408889634f, a->cache.k_exp);
   p.v_scale = std::ldexp(1.0f, a->cache.v_exp);
   char* ws = static_cast<char*>(a->workspace);
-  p.rows_from = 0; p.rows_to = 0x7fffffffffffLL;
   p.wait_limit = fwd::g_wait_limit;
   p.withhold = fwd::g_withhold_tile;
   p.status = reinterpret_cast<int32_t*>(ws);
@@ -652,10 +670,7 @@ sol_status_t sol_attn_cache_attention(const sol_attn_cache_args* a) {
   int n = 0;
   auto typed = [&](auto zero) {
     using T = decltype(zero);
-    const bool eight = (long long)a->max_q * p.group <= 8;
-    if (a->cache.d == 128)
-      return eight ? cache::run<T, 128, 1>(p, sms, stream, &n) : cache::run<T, 128, 2>(p, sms, stream, &n);
-    return eight ? cache::run<T, 64, 1>(p, sms, stream, &n) : cache::run<T, 64, 2>(p, sms, stream, &n);
+    return a->cache.d == 128 ? cache::run<T, 128>(p, a->max_q, a->type, sms, stream, &n) : cache::run<T, 64>(p, a->max_q, a->type, sms, stream, &n);
   };
   const cudaError_t e = a->type == SOL_TYPE_BF16 ? typed(__nv_bfloat16{}) : typed(__half{});
   count_launches(n);

@@ -7,6 +7,16 @@
 namespace sol {
 namespace cache {
 
+// Weights are 2^(x - m + kShift) with x the logit times log2(e) and m a maximum of earlier keys, which is replaced once a weight would
+// pass 2^kMost: fp16 holds them to 2^-12 down to 2^-25 of the largest, and is off by 2^-36 of it at most below.
+constexpr float kShift = 11.f, kMost = 15.f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// The workspace: status word, a record per block, two partial results per block.  One kernel at a time has it: it is laid out for each.
+constexpr size_t kRecordsAt = 1024;
+constexpr int kMostBlocks = 4 * 160, kMostChunkBlocks = 160;   // of the kernel for few queries, of the other
+constexpr int kChunkRows = 256;                  // rows of a block of the other
+
 // An item of which a block had the last piece and others the rest: the first of them (-1: there is no such item), and where its rows
 // belong.
 struct alignas(32) Record { int from, head, tile, queries, first, pad0, pad1, pad2; };
@@ -44,14 +54,30 @@ __device__ __forceinline__ Request request_at(const AttnParams& p, int b) {
 // shares of the steps, the first ones one more where they do not come out even: every block has the same to do, however ragged the
 // batch, and an item is cut into as many pieces as there are blocks on it.  A piece that is not a whole item is left in `parts`
 // and joined by a second kernel, in order.
-struct Work {
-  int tiles, steps;                              // of a request: row tiles per head, steps per item (at least one)
-  __device__ Work(const AttnParams& p, const Request& r, int rows, int step) {
+template <int kRows, int kStep>
+struct Tiles {
+  // Row tiles of a request, per head; none if the request is another kernel's.
+  __device__ static int count(const AttnParams& p, const Request& r) {
     const long long all = (long long)r.queries * p.group;
-    tiles = all < p.rows_from || all > p.rows_to ? 0 : (int)(((uint32_t)all + rows - 1) / rows);     // (not this kernel's request: none)
-    steps = max(1, (r.keys + step - 1) / step);
+    return all < p.rows_from || all > p.rows_to ? 0 : (int)(((uint32_t)all + kRows - 1) / kRows);
   }
-  __device__ long long total(int heads) const { return (long long)tiles * heads * steps; }
+  // Steps of a tile (at least one): up to the last key that its last row sees.
+  __device__ static int steps(const AttnParams& p, const Request& r, int tile) {
+    int sees = r.keys;
+    if (p.causal) {
+      const int last = min((tile + 1) * kRows, r.queries * p.group) - 1;
+      sees = min(sees, r.keys - r.queries + last / p.group + 1);
+    }
+    return max(1, (sees + kStep - 1) / kStep);
+  }
+  // Steps of all tiles of a head.
+  __device__ static long long per_head(const AttnParams& p, const Request& r) {
+    const int n = count(p, r);
+    if (!p.causal || n <= 1) return n ? (long long)n * steps(p, r, n - 1) : 0;
+    long long s = 0;
+    for (int i = 0; i < n; ++i) s += steps(p, r, i);
+    return s;
+  }
 };
 
 // a / b for a >= 0, b > 0; 32 bits do it nearly always, and are several times as fast.
@@ -76,17 +102,56 @@ struct Start {                                   // where a block begins
   long long base;                                // its first step
 };
 
+// The pieces of a block's share, one after the other.
+template <class Tiling>
+struct Pieces {
+  Request r;
+  int b, head, tile, s_begin, s_end, steps;      // the piece: steps [s_begin, s_end) of `steps`
+  int more;                                      // there is one
+  long long w, w_end, base, per_head, item_begin;
+  __device__ void start(const AttnParams& p, const Start& at, long long begin, long long end) {
+    r = at.request; b = at.index; base = at.base; w = begin; w_end = end;
+    per_head = Tiling::per_head(p, r);
+    head = tile = s_begin = s_end = steps = 0;
+    item_begin = 0;
+  }
+  __device__ bool next(const AttnParams& p) {
+    if (w >= w_end) return false;
+    if (s_end != 0 && s_end == steps && w < base + per_head * (head + 1)) {    // the head's next tile
+      ++tile;
+      item_begin = w;
+    } else {
+      while (w >= base + per_head * p.Hk) {      // the next request with work
+        base += per_head * p.Hk;
+        r = request_at(p, ++b);
+        per_head = Tiling::per_head(p, r);
+      }
+      head = (int)quotient(w - base, per_head);
+      item_begin = base + per_head * head;
+      tile = 0;
+      for (int n; w >= item_begin + (n = Tiling::steps(p, r, tile)); ++tile) item_begin += n;
+    }
+    steps = Tiling::steps(p, r, tile);
+    s_begin = (int)(w - item_begin);
+    s_end = (int)min((long long)steps, w_end - item_begin);
+    w = item_begin + s_end;
+    return true;
+  }
+  __device__ bool begins() const { return s_begin == 0; }
+  __device__ bool ends() const { return s_end == steps; }
+};
+
 // The sum of the requests' work, and, where `c` has a share of it, where that begins (in `start`, shared memory).  The whole block
 // calls it; `sums`: shared memory, a word per warp.
-template <int kThreads>
-__device__ Shares find_share(const AttnParams& p, int rows, int step, long long c, long long* sums, Start* start) {
+template <int kThreads, class Tiling>
+__device__ Shares find_share(const AttnParams& p, long long c, long long* sums, Start* start) {
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
   long long all = 0, x = 0, n = 0;
   Request r{0, 0, 0};
   auto scan = [&](int b0) {                      // of requests b0 ...: x the sum up to this thread's, n its own; returns that of all
     r = Request{0, 0, 0};
     n = 0;
-    if (b0 + tid < p.requests) { r = request_at(p, b0 + tid); n = Work(p, r, rows, step).total(p.Hk); }
+    if (b0 + tid < p.requests) { r = request_at(p, b0 + tid); n = Tiling::per_head(p, r) * p.Hk; }
     x = n;
     for (int o = 1; o < 32; o *= 2) {
       const long long y = __shfl_up_sync(0xffffffffu, x, o);
@@ -115,6 +180,9 @@ __device__ Shares find_share(const AttnParams& p, int rows, int step, long long 
   }
   return sh;
 }
+
+// The kernel for many queries (cache_attention_chunk.cu); `grid` gets its blocks.
+cudaError_t launch_chunk(const AttnParams& p, int d, int type, int sms, cudaStream_t stream, int* grid);
 
 }  // namespace cache
 }  // namespace sol
