@@ -8,8 +8,8 @@
 //   softmax  (warps 0-3: tile A, 4-7: tile B) thread = row, with all 128 scores of a tile of keys in registers; at the start of a piece it
 //            puts the row's queries into shared memory, scaled by a power of two so that fp16 holds them
 //   mma      (warp 8)
-//   widen    (warps 9-15) units of 16 tokens in turn, the next one's bytes on their way meanwhile: fp16 tiles in a ring of five
-//            slots, K0 V0 K1 V1 ..., in the 128-byte swizzle that the tensor core reads
+//   widen    (warps 9-15) units of 16 tokens in turn, the next one's bytes on their way to shared memory meanwhile: fp16 tiles in a ring
+//            of four slots, K0 V0 K1 V1 ..., in the 128-byte swizzle that the tensor core reads
 // The cache's values are exact in fp16, so K and V enter the products unrounded.
 //
 // TMEM: S_A [0, 128)  S_B [128, 256)  O_A [256, 256 + d)  O_B [256 + d, 256 + 2 d).  Every wait is bounded.
@@ -30,7 +30,7 @@ using fwd::tmem_ld_cols;
 constexpr int kThreads = 512;
 constexpr int kTileRows = 128, kRows = kChunkRows, kCols = 128;   // of a tile, of a block; keys of a step
 constexpr int kUnits = kCols / kUnit;
-constexpr int kSlots = 5;
+constexpr int kSlots = 4;
 constexpr int kWarpMma = 8, kWarpWiden = 9, kWideners = 7;
 constexpr int kTmemS = 0, kTmemO = 256;
 constexpr int kRegsSoftmax = 200, kRegsOther = 56, kRegsLaunch = 128;   // registers per thread of the roles, and at launch
@@ -44,12 +44,13 @@ struct Cfg {
   static constexpr int kTileBytes = kCols * D * 2;         // a query, K or V tile
   static constexpr int kBoxBytes = kCols * 128;            // 64 channels of it
   static constexpr int kPartFloats = kRows * (D + 2);
-  static constexpr size_t kSmem = 1024 + (2 + kSlots) * kTileBytes;
+  static constexpr size_t kSmem = 1024 + (2 + kSlots) * kTileBytes + kWideners * 2 * Unit<D>::kBytes;
 };
 
 struct Shared {
   uint64_t q_full[2], q_empty[2];                // per row tile
   uint64_t kv_full[kSlots], kv_empty[kSlots];
+  uint64_t raw_full[kWideners][2];               // a unit's bytes are there
   uint64_t s_full[2];                            // scores of a tile are in TMEM
   uint64_t p_full[2][2];                         // first / second half of the columns of P are in TMEM
   uint64_t o_full[2], o_free[2];                 // accumulator complete / read
@@ -108,121 +109,134 @@ __device__ __forceinline__ void put_chunk(unsigned char* tile, int row, int x, u
 }
 
 template <int D>
-__device__ void widen_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at, unsigned char* sKV, int me, int lane) {
+__device__ void widen_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at, unsigned char* sKV, unsigned char* raw_ring, int me, int lane) {
   using C = Cfg<D>;
   using U = Unit<D>;
-  constexpr int kHalfBytes = 16 * D / 32;        // of a lane, both halves of a unit's keys or values: 16 (d = 64 8)
   const int g = lane / 4, t = lane % 4;
-  uint32_t m = 0;                                // tiles of the ring so far
-  // A warp's tasks are units me, me + 7, ... of the units of all tiles one after the other.  They are walked one ahead: the bytes
-  // of the next one are in registers, or on their way there, while one is widened.
-  struct Task { uint32_t m; int unit, valid; bool values; };
-  Task next{0, 0, 0, false};
-  uint4 raw{0, 0, 0, 0}, raw2{0, 0, 0, 0};
-  uint32_t scale = 0;
-  int step = 0, side = 0, unit = me;             // where the walk is in the piece
+  // A warp's tasks are units me, me + 7, ... of the units of all key tiles one after the other, keys and values of each.  They are walked
+  // two ahead: while one is widened, the bytes of the next are on their way to shared memory, and the page of the one behind.
+  struct Task { uint32_t tile, offset; int unit, valid, page; };               // offset: of the unit in a page's bytes
+  constexpr uint32_t kNone = 0xffffffffu;
+  uint32_t tiles = 0, issued = 0, done = 0;      // key tiles walked over; copies so far, and those waited for
+  int step = 0, unit = me;                       // where the walk is in the piece
   bool more = next_piece(at, p, lane);
   if (more) step = at.s_begin;
-  auto advance = [&] {                           // to the next task, and its loads
+  const uint32_t unit_mask = (1u << (p.page_shift - 4)) - 1, head_bytes = (uint32_t)U::kBytes << (p.page_shift - 4);
+  auto walk = [&] {
     while (more && unit >= kUnits) {             // the next tile
       unit -= kUnits;
-      ++m;
-      if (++side == 2) {
-        side = 0;
-        if (++step == at.s_end) {
-          more = next_piece(at, p, lane);
-          if (more) step = at.s_begin;
-        }
+      ++tiles;
+      if (++step == at.s_end) {
+        more = next_piece(at, p, lane);
+        if (more) step = at.s_begin;
       }
     }
-    if (!more) return false;
-    const int u = step * kUnits + unit, keys = at.r.keys - u * kUnit;
-    int page = -1;
-    if (keys > 0) {
-      page = p.tables[at.b * p.table_stride + (u >> (p.page_shift - 4))];
-      if (page >= p.pages) page = -1;
-      if (page < 0) *(volatile int*)&sm.missing = 1;
+    Task task{kNone, 0, 0, 0, -1};
+    if (more) {
+      const int u = step * kUnits + unit;
+      task.tile = tiles;
+      task.offset = at.head * head_bytes + ((uint32_t)u & unit_mask) * U::kBytes;
+      task.unit = unit;
+      task.valid = min(at.r.keys - u * kUnit, kUnit);
+      if (task.valid > 0) task.page = p.tables[at.b * p.table_stride + (u >> (p.page_shift - 4))];
+      unit += kWideners;
     }
-    next = Task{m, unit, page >= 0 ? min(keys, kUnit) : 0, side == 1};
-    if (page >= 0) {
-      const int in_page = u & ((1 << (p.page_shift - 4)) - 1);
-      const unsigned char* src =
-          p.data + (((size_t)page * p.Hk + at.head << (p.page_shift - 4)) + in_page) * U::kBytes + (side ? U::kValues : U::kKeys);
-      if constexpr (D == 128) {
-        raw = __ldg(reinterpret_cast<const uint4*>(src) + lane);
-        raw2 = __ldg(reinterpret_cast<const uint4*>(src) + 32 + lane);
-      } else {
-        const uint2 a = __ldg(reinterpret_cast<const uint2*>(src) + lane), b = __ldg(reinterpret_cast<const uint2*>(src) + 32 + lane);
-        raw = make_uint4(a.x, a.y, b.x, b.y);
-      }
-      const unsigned char* sc = src + (side ? U::kValueScales - U::kValues : U::kKeyScales - U::kKeys);
-      if (side) scale = __ldg(reinterpret_cast<const uint32_t*>(sc) + (D == 128 ? g : g / 2) * 4 + t);
-      else if constexpr (D == 128) scale = __ldg(reinterpret_cast<const uint32_t*>(sc) + lane);
-      else scale = __ldg(reinterpret_cast<const uint16_t*>(sc) + lane);
-    }
-    unit += kWideners;
-    return true;
+    return task;
   };
-  bool have = advance();
-  while (have) {
-    const Task task = next;
-    const uint32_t slot = task.m % kSlots;
-    uint32_t w[2][4];                            // halves of the unit
-    if constexpr (D == 128) {
-      w[0][0] = raw.x; w[0][1] = raw.y; w[0][2] = raw.z; w[0][3] = raw.w;
-      w[1][0] = raw2.x; w[1][1] = raw2.y; w[1][2] = raw2.z; w[1][3] = raw2.w;
-    } else {
-      w[0][0] = raw.x; w[0][1] = raw.y; w[1][0] = raw.z; w[1][1] = raw.w;
+  auto issue = [&](Task& task) {
+    if (task.tile == kNone) return;
+    const bool has = task.valid > 0 && task.page >= 0 && task.page < p.pages;
+    if (!has && task.valid > 0) { *(volatile int*)&sm.missing = 1; task.valid = 0; }
+    if (lane == 0) {
+      uint64_t* bar = &sm.raw_full[me][issued & 1];
+      mbar_arrive_expect_tx(bar, has ? U::kBytes : 0);
+      if (has)
+        bulk_load_1d(raw_ring + (issued & 1) * U::kBytes, p.data + (size_t)(uint32_t)task.page * p.Hk * head_bytes + task.offset, U::kBytes, bar);
     }
-    uint32_t sc = scale;
-    have = advance();
-    if (!WAIT_ALL(&sm.kv_empty[slot], ((task.m / kSlots) & 1) ^ 1)) { if (lane == 0) flag_timeout(sm, p); return; }
-    unsigned char* tile = sKV + slot * C::kTileBytes;
+    ++issued;
+  };
+  Task task = walk();
+  issue(task);
+  Task next = walk();
+  issue(next);
+  Task behind = walk();
+  bool ok = true;
+  while (task.tile != kNone) {
+    const unsigned char* raw = raw_ring + (done & 1) * U::kBytes;
+    if (!WAIT_ALL(&sm.raw_full[me][done & 1], (done >> 1) & 1)) { ok = false; break; }
+    ++done;
     const int row0 = task.unit * kUnit;
-    if (task.values) {
-      // tokens 8 h + 2 t + e of the unit, channels g d / 8 ...: d / 64 words of 8 channels each
-#pragma unroll
-      for (int x = 0; x < 4; ++x)                // what no row may see is multiplied by zero
-        if (2 * t + (x & 1) + 8 * (x >> 1) >= task.valid) sc &= ~(0xffu << (8 * x));
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const __half2 both = scales2(h ? sc >> 16 : sc & 0xffff), of[2] = {__low2half2(both), __high2half2(both)};
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-          for (int y = 0; y < D / 64; ++y) {
-            uint32_t c[4];
-            codes8(task.valid ? w[h][e * (D / 64) + y] : 0u, c);
-#pragma unroll
-            for (int x = 0; x < 4; ++x) c[x] = bits(__hmul2(half2_of(c[x]), of[e]));
-            put_chunk<D>(tile, row0 + 8 * h + 2 * t + e, g * (D / 64) + y, make_uint4(c[0], c[1], c[2], c[3]));
-          }
-      }
-    } else {
-      // tokens g and g + 8, channels t d / 4 ...: d / 32 words of 8 channels each
+    {                                            // keys: tokens g and g + 8, channels t d / 4 ...: d / 32 words of 8 channels each
+      const uint32_t m = 2 * task.tile, slot = m % kSlots;
+      if (!WAIT_ALL(&sm.kv_empty[slot], ((m / kSlots) & 1) ^ 1)) { ok = false; break; }
+      unsigned char* tile = sKV + slot * C::kTileBytes;
+      uint32_t sc;
+      if constexpr (D == 128) sc = *reinterpret_cast<const uint32_t*>(raw + U::kKeyScales + lane * 4);
+      else sc = *reinterpret_cast<const uint16_t*>(raw + U::kKeyScales + lane * 2);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
+        uint32_t w[D / 32];
         __half2 of[2];
         if constexpr (D == 128) {
+          *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(raw + U::kKeys + (h * 32 + lane) * 16);
           const __half2 both = scales2(h ? sc >> 16 : sc & 0xffff);
           of[0] = __low2half2(both); of[1] = __high2half2(both);
         } else {
+          *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(raw + U::kKeys + (h * 32 + lane) * 8);
           const __half2 both = scales2(sc);
           of[0] = of[1] = h ? __high2half2(both) : __low2half2(both);
         }
 #pragma unroll
         for (int y = 0; y < D / 32; ++y) {
           uint32_t c[4];
-          codes8(w[h][y], c);
+          codes8(w[y], c);
 #pragma unroll
           for (int x = 0; x < 4; ++x) c[x] = bits(__hmul2(half2_of(c[x]), of[y / 2]));
           put_chunk<D>(tile, row0 + 8 * h + g, t * (D / 32) + y, make_uint4(c[0], c[1], c[2], c[3]));
         }
       }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0 && (int)m != p.withhold) mbar_arrive(&sm.kv_full[slot]);   // (a test withholds a tile's)
     }
-    fence_proxy_async_smem();
-    __syncwarp();
-    if (lane == 0 && (int)task.m != p.withhold) mbar_arrive(&sm.kv_full[slot]);  // (a test withholds a tile's)
+    {                                            // values: tokens 8 h + 2 t + e, channels g d / 8 ...: d / 64 words of 8 channels each
+      const uint32_t m = 2 * task.tile + 1, slot = m % kSlots;
+      if (!WAIT_ALL(&sm.kv_empty[slot], ((m / kSlots) & 1) ^ 1)) { ok = false; break; }
+      unsigned char* tile = sKV + slot * C::kTileBytes;
+      uint32_t sc = *reinterpret_cast<const uint32_t*>(raw + U::kValueScales + ((D == 128 ? g : g / 2) * 4 + t) * 4);
+#pragma unroll
+      for (int x = 0; x < 4; ++x)                // what no row may see is multiplied by zero
+        if (2 * t + (x & 1) + 8 * (x >> 1) >= task.valid) sc &= ~(0xffu << (8 * x));
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t w[D / 32];
+        if constexpr (D == 128) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(raw + U::kValues + (h * 32 + lane) * 16);
+        else *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(raw + U::kValues + (h * 32 + lane) * 8);
+        const __half2 both = scales2(h ? sc >> 16 : sc & 0xffff), of[2] = {__low2half2(both), __high2half2(both)};
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int y = 0; y < D / 64; ++y) {
+            uint32_t c[4];
+            codes8(w[e * (D / 64) + y], c);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) c[x] = bits(__hmul2(half2_of(c[x]), of[e]));
+            put_chunk<D>(tile, row0 + 8 * h + 2 * t + e, g * (D / 64) + y, make_uint4(c[0], c[1], c[2], c[3]));
+          }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0 && (int)m != p.withhold) mbar_arrive(&sm.kv_full[slot]);
+    }
+    task = next;
+    next = behind;
+    issue(next);
+    behind = walk();
+  }
+  if (!ok) {                                     // no copy is left in flight
+    if (lane == 0) flag_timeout(sm, p);
+    int never = 0;
+    for (; done < issued; ++done) mbar_wait_inline(&sm.raw_full[me][done & 1], (done >> 1) & 1, &never, p.wait_limit);
   }
 }
 
@@ -538,6 +552,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_chunk_kernel(cons
       mbar_init(&sm.p_full[s][0], 4); mbar_init(&sm.p_full[s][1], 4);
       mbar_init(&sm.o_full[s], 1); mbar_init(&sm.o_free[s], 4);
     }
+    for (int i = 0; i < kWideners; ++i) { mbar_init(&sm.raw_full[i][0], 1); mbar_init(&sm.raw_full[i][1], 1); }
     mbar_init(&sm.mma_drain, 1);
     fence_mbar_init();
   }
@@ -558,7 +573,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_chunk_kernel(cons
     } else {
       set_max_registers_down<kRegsOther>();
       if (warp == kWarpMma) mma_role<D>(sm, p, sm.pieces[warp], sQ, sKV, tmem, lane, shares);
-      else widen_role<D>(sm, p, sm.pieces[warp], sKV, warp - kWarpWiden, lane);
+      else widen_role<D>(sm, p, sm.pieces[warp], sKV, sKV + kSlots * C::kTileBytes + (warp - kWarpWiden) * 2 * Unit<D>::kBytes,
+                         warp - kWarpWiden, lane);
     }
   } else if (threadIdx.x == 0) {
     p.records[blockIdx.x] = Record{-1, 0, 0, 0, 0, 0, 0, 0};
