@@ -8,8 +8,8 @@
 //   softmax  (warps 0-3: tile A, 4-7: tile B) thread = row, with all 128 scores of a tile of keys in registers; at the start of a piece it
 //            puts the row's queries into shared memory, scaled by a power of two so that fp16 holds them
 //   mma      (warp 8)
-//   widen    (warps 9-15) units of 16 tokens in turn, the next one's bytes on their way to shared memory meanwhile: fp16 tiles in a ring
-//            of four slots, K0 V0 K1 V1 ..., in the 128-byte swizzle that the tensor core reads
+//   loader   (warp 9) the cache's units of 16 tokens into a ring of 14
+//   widen    (warps 10-15) units to fp16 tiles in a ring of four slots, K0 V0 K1 V1 ..., in the 128-byte swizzle that the tensor core reads
 // The cache's values are exact in fp16, so K and V enter the products unrounded.
 //
 // TMEM: S_A [0, 128)  S_B [128, 256)  O_A [256, 256 + d)  O_B [256 + d, 256 + 2 d).  Every wait is bounded.
@@ -31,7 +31,8 @@ constexpr int kThreads = 512;
 constexpr int kTileRows = 128, kRows = kChunkRows, kCols = 128;   // of a tile, of a block; keys of a step
 constexpr int kUnits = kCols / kUnit;
 constexpr int kSlots = 4;
-constexpr int kWarpMma = 8, kWarpWiden = 9, kWideners = 7;
+constexpr int kWarpMma = 8, kWarpLoader = 9, kWarpWiden = 10, kWideners = 6;
+constexpr int kRaw = 14;                         // units in the raw ring
 constexpr int kTmemS = 0, kTmemO = 256;
 constexpr int kRegsSoftmax = 200, kRegsOther = 56, kRegsLaunch = 128;   // registers per thread of the roles, and at launch
 static_assert(8 * kRegsSoftmax + 8 * kRegsOther <= 16 * kRegsLaunch, "a warpgroup would wait for registers without end");
@@ -44,13 +45,14 @@ struct Cfg {
   static constexpr int kTileBytes = kCols * D * 2;         // a query, K or V tile
   static constexpr int kBoxBytes = kCols * 128;            // 64 channels of it
   static constexpr int kPartFloats = kRows * (D + 2);
-  static constexpr size_t kSmem = 1024 + (2 + kSlots) * kTileBytes + kWideners * 2 * Unit<D>::kBytes;
+  static constexpr size_t kSmem = 1024 + (2 + kSlots) * kTileBytes + kRaw * Unit<D>::kBytes;
 };
 
 struct Shared {
   uint64_t q_full[2], q_empty[2];                // per row tile
   uint64_t kv_full[kSlots], kv_empty[kSlots];
-  uint64_t raw_full[kWideners][2];               // a unit's bytes are there
+  uint64_t raw_full[kRaw], raw_empty[kRaw];      // a unit's bytes are there; its keys and its values are widened
+  int raw_valid[kRaw];                           // tokens of it that there are
   uint64_t s_full[2];                            // scores of a tile are in TMEM
   uint64_t p_full[2][2];                         // first / second half of the columns of P are in TMEM
   uint64_t o_full[2], o_free[2];                 // accumulator complete / read
@@ -108,68 +110,106 @@ __device__ __forceinline__ void put_chunk(unsigned char* tile, int row, int x, u
   *reinterpret_cast<uint4*>(tile + (x >> 3) * Cfg<D>::kBoxBytes + row * 128 + (((x & 7) ^ (row & 7)) << 4)) = v;
 }
 
+// Units of 16 tokens into the raw ring, in order, a step's eight by a lane each.
 template <int D>
-__device__ void widen_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at, unsigned char* sKV, unsigned char* raw_ring, int me, int lane) {
+__device__ void loader_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at, unsigned char* sRaw, int lane) {
+  using U = Unit<D>;
+  const uint32_t unit_mask = (1u << (p.page_shift - 4)) - 1, head_bytes = (uint32_t)U::kBytes << (p.page_shift - 4);
+  uint32_t n = lane;                             // this lane's unit, counted over all pieces
+  bool ok = true;
+  while (ok && next_piece(at, p, lane)) {
+    const int32_t* table = p.tables + at.b * p.table_stride;
+    const int keys = at.r.keys, steps_end = at.s_end;
+    const uint32_t head_at = at.head * head_bytes;
+    auto page_of = [&](int step) {
+      const int u = step * kUnits + lane;
+      return lane < kUnits && step < steps_end && u * kUnit < keys ? table[u >> (p.page_shift - 4)] : -1;
+    };
+    int page = page_of(at.s_begin);
+    for (int step = at.s_begin; ok && step < steps_end; ++step, n += kUnits) {
+      const int u = step * kUnits + lane;
+      const int next_page = page_of(step + 1);
+      bool mine = true;
+      for (int x = 0; x < kUnits; ++x) {         // one after the other: the first need not wait for room for the last
+        if (lane == x) {
+          const uint32_t slot = n % kRaw;
+          mine = WAIT(&sm.raw_empty[slot], ((n / kRaw) & 1) ^ 1);
+          if (mine) {
+            int valid = max(0, min(keys - u * kUnit, kUnit));
+            if (valid > 0 && (page < 0 || page >= p.pages)) { *(volatile int*)&sm.missing = 1; valid = 0; }
+            *(volatile int*)&sm.raw_valid[slot] = valid;
+            mbar_arrive_expect_tx(&sm.raw_full[slot], valid ? U::kBytes : 0);
+            if (valid)
+              bulk_load_1d(sRaw + slot * U::kBytes, p.data + (size_t)(uint32_t)page * p.Hk * head_bytes + head_at + ((uint32_t)u & unit_mask) * U::kBytes,
+                           U::kBytes, &sm.raw_full[slot]);
+          }
+        }
+        __syncwarp();
+      }
+      ok = __all_sync(kAll, mine);
+      page = next_page;
+    }
+  }
+  if (!ok) {
+    if (lane == 0) flag_timeout(sm, p);
+    // let copies that are still in flight land before the block's shared memory goes away (not cut short by the flag)
+    int never = 0;
+    if (lane < kUnits)
+      for (int back = 1; back <= 2 && n >= (uint32_t)(back * kUnits); ++back) {
+        const uint32_t x = n - back * kUnits;
+        mbar_wait_inline(&sm.raw_full[x % kRaw], (x / kRaw) & 1, &never, p.wait_limit);
+      }
+  }
+}
+
+// Raw units to fp16 tiles.  The tasks, eight units of keys and eight of values for each tile of keys, lie one after the other, and
+// kWideners warps take them in turn.
+template <int D>
+__device__ void widen_role(Shared& sm, const AttnParams& p, uint32_t tiles, unsigned char* sKV, unsigned char* sRaw, int me, int lane) {
   using C = Cfg<D>;
   using U = Unit<D>;
   const int g = lane / 4, t = lane % 4;
-  // A warp's tasks are units me, me + 7, ... of the units of all key tiles one after the other, keys and values of each.  They are walked
-  // two ahead: while one is widened, the bytes of the next are on their way to shared memory, and the page of the one behind.
-  struct Task { uint32_t tile, offset; int unit, valid, page; };               // offset: of the unit in a page's bytes
-  constexpr uint32_t kNone = 0xffffffffu;
-  uint32_t tiles = 0, issued = 0, done = 0;      // key tiles walked over; copies so far, and those waited for
-  int step = 0, unit = me;                       // where the walk is in the piece
-  bool more = next_piece(at, p, lane);
-  if (more) step = at.s_begin;
-  const uint32_t unit_mask = (1u << (p.page_shift - 4)) - 1, head_bytes = (uint32_t)U::kBytes << (p.page_shift - 4);
-  auto walk = [&] {
-    while (more && unit >= kUnits) {             // the next tile
-      unit -= kUnits;
-      ++tiles;
-      if (++step == at.s_end) {
-        more = next_piece(at, p, lane);
-        if (more) step = at.s_begin;
-      }
-    }
-    Task task{kNone, 0, 0, 0, -1};
-    if (more) {
-      const int u = step * kUnits + unit;
-      task.tile = tiles;
-      task.offset = at.head * head_bytes + ((uint32_t)u & unit_mask) * U::kBytes;
-      task.unit = unit;
-      task.valid = min(at.r.keys - u * kUnit, kUnit);
-      if (task.valid > 0) task.page = p.tables[at.b * p.table_stride + (u >> (p.page_shift - 4))];
-      unit += kWideners;
-    }
-    return task;
-  };
-  auto issue = [&](Task& task) {
-    if (task.tile == kNone) return;
-    const bool has = task.valid > 0 && task.page >= 0 && task.page < p.pages;
-    if (!has && task.valid > 0) { *(volatile int*)&sm.missing = 1; task.valid = 0; }
-    if (lane == 0) {
-      uint64_t* bar = &sm.raw_full[me][issued & 1];
-      mbar_arrive_expect_tx(bar, has ? U::kBytes : 0);
-      if (has)
-        bulk_load_1d(raw_ring + (issued & 1) * U::kBytes, p.data + (size_t)(uint32_t)task.page * p.Hk * head_bytes + task.offset, U::kBytes, bar);
-    }
-    ++issued;
-  };
-  Task task = walk();
-  issue(task);
-  Task next = walk();
-  issue(next);
-  Task behind = walk();
   bool ok = true;
-  while (task.tile != kNone) {
-    const unsigned char* raw = raw_ring + (done & 1) * U::kBytes;
-    if (!WAIT_ALL(&sm.raw_full[me][done & 1], (done >> 1) & 1)) { ok = false; break; }
-    ++done;
-    const int row0 = task.unit * kUnit;
-    {                                            // keys: tokens g and g + 8, channels t d / 4 ...: d / 32 words of 8 channels each
-      const uint32_t m = 2 * task.tile, slot = m % kSlots;
-      if (!WAIT_ALL(&sm.kv_empty[slot], ((m / kSlots) & 1) ^ 1)) { ok = false; break; }
-      unsigned char* tile = sKV + slot * C::kTileBytes;
+  for (uint32_t task = me; task < 2 * kUnits * tiles; task += kWideners) {
+    const uint32_t m = task / kUnits, slot = m % kSlots;         // tile of the ring
+    const bool values = m & 1;
+    const uint32_t unit = task % kUnits, n = m / 2 * kUnits + unit, raw_slot = n % kRaw;
+    if (!WAIT_ALL(&sm.raw_full[raw_slot], (n / kRaw) & 1)) { ok = false; break; }
+    if (!WAIT_ALL(&sm.kv_empty[slot], ((m / kSlots) & 1) ^ 1)) { ok = false; break; }
+    const unsigned char* raw = sRaw + raw_slot * U::kBytes;
+    unsigned char* tile = sKV + slot * C::kTileBytes;
+    const int row0 = unit * kUnit;
+    if (values) {                                // tokens 8 h + 2 t + e, channels g d / 8 ...: d / 64 words of 8 channels each
+      const int valid = *(volatile int*)&sm.raw_valid[raw_slot];
+      uint32_t sc = *reinterpret_cast<const uint32_t*>(raw + U::kValueScales + ((D == 128 ? g : g / 2) * 4 + t) * 4);
+      if (valid < kUnit) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x)              // what no row may see is multiplied by zero
+          if (2 * t + (x & 1) + 8 * (x >> 1) >= valid) sc &= ~(0xffu << (8 * x));
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t w[D / 32];
+        if constexpr (D == 128) {
+          // (odd lanes g write their two chunks the other way round: with that, eight lanes write to eight different groups of banks)
+          const uint4 x = *reinterpret_cast<const uint4*>(raw + U::kValues + (h * 32 + lane) * 16);
+          w[0] = g & 1 ? x.y : x.x; w[1] = g & 1 ? x.x : x.y; w[2] = g & 1 ? x.w : x.z; w[3] = g & 1 ? x.z : x.w;
+        } else {
+          *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(raw + U::kValues + (h * 32 + lane) * 8);
+        }
+        const __half2 both = scales2(h ? sc >> 16 : sc & 0xffff), of[2] = {__low2half2(both), __high2half2(both)};
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int y = 0; y < D / 64; ++y) {
+            uint32_t c[4];
+            codes8(w[e * (D / 64) + y], c);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) c[x] = bits(__hmul2(half2_of(c[x]), of[e]));
+            put_chunk<D>(tile, row0 + 8 * h + 2 * t + e, g * (D / 64) + (D == 128 ? y ^ (g & 1) : y), make_uint4(c[0], c[1], c[2], c[3]));
+          }
+      }
+    } else {                                     // tokens 8 h + g, channels t d / 4 ...: d / 32 words of 8 channels each
       uint32_t sc;
       if constexpr (D == 128) sc = *reinterpret_cast<const uint32_t*>(raw + U::kKeyScales + lane * 4);
       else sc = *reinterpret_cast<const uint16_t*>(raw + U::kKeyScales + lane * 2);
@@ -178,9 +218,12 @@ __device__ void widen_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at, 
         uint32_t w[D / 32];
         __half2 of[2];
         if constexpr (D == 128) {
-          *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(raw + U::kKeys + (h * 32 + lane) * 16);
+          // (lanes of the second box write the second half of their channels first: eight groups of banks again)
+          const uint4 x = *reinterpret_cast<const uint4*>(raw + U::kKeys + (h * 32 + lane) * 16);
           const __half2 both = scales2(h ? sc >> 16 : sc & 0xffff);
-          of[0] = __low2half2(both); of[1] = __high2half2(both);
+          w[0] = t & 2 ? x.z : x.x; w[1] = t & 2 ? x.w : x.y; w[2] = t & 2 ? x.x : x.z; w[3] = t & 2 ? x.y : x.w;
+          of[0] = t & 2 ? __high2half2(both) : __low2half2(both);
+          of[1] = t & 2 ? __low2half2(both) : __high2half2(both);
         } else {
           *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(raw + U::kKeys + (h * 32 + lane) * 8);
           const __half2 both = scales2(sc);
@@ -192,52 +235,18 @@ __device__ void widen_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at, 
           codes8(w[y], c);
 #pragma unroll
           for (int x = 0; x < 4; ++x) c[x] = bits(__hmul2(half2_of(c[x]), of[y / 2]));
-          put_chunk<D>(tile, row0 + 8 * h + g, t * (D / 32) + y, make_uint4(c[0], c[1], c[2], c[3]));
+          put_chunk<D>(tile, row0 + 8 * h + g, t * (D / 32) + (D == 128 ? y ^ (t & 2) : y), make_uint4(c[0], c[1], c[2], c[3]));
         }
       }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0 && (int)m != p.withhold) mbar_arrive(&sm.kv_full[slot]);   // (a test withholds a tile's)
     }
-    {                                            // values: tokens 8 h + 2 t + e, channels g d / 8 ...: d / 64 words of 8 channels each
-      const uint32_t m = 2 * task.tile + 1, slot = m % kSlots;
-      if (!WAIT_ALL(&sm.kv_empty[slot], ((m / kSlots) & 1) ^ 1)) { ok = false; break; }
-      unsigned char* tile = sKV + slot * C::kTileBytes;
-      uint32_t sc = *reinterpret_cast<const uint32_t*>(raw + U::kValueScales + ((D == 128 ? g : g / 2) * 4 + t) * 4);
-#pragma unroll
-      for (int x = 0; x < 4; ++x)                // what no row may see is multiplied by zero
-        if (2 * t + (x & 1) + 8 * (x >> 1) >= task.valid) sc &= ~(0xffu << (8 * x));
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t w[D / 32];
-        if constexpr (D == 128) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(raw + U::kValues + (h * 32 + lane) * 16);
-        else *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(raw + U::kValues + (h * 32 + lane) * 8);
-        const __half2 both = scales2(h ? sc >> 16 : sc & 0xffff), of[2] = {__low2half2(both), __high2half2(both)};
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-          for (int y = 0; y < D / 64; ++y) {
-            uint32_t c[4];
-            codes8(w[e * (D / 64) + y], c);
-#pragma unroll
-            for (int x = 0; x < 4; ++x) c[x] = bits(__hmul2(half2_of(c[x]), of[e]));
-            put_chunk<D>(tile, row0 + 8 * h + 2 * t + e, g * (D / 64) + y, make_uint4(c[0], c[1], c[2], c[3]));
-          }
-      }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0 && (int)m != p.withhold) mbar_arrive(&sm.kv_full[slot]);
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      if ((int)m != p.withhold) mbar_arrive(&sm.kv_full[slot]);  // (a test withholds a tile's)
+      mbar_arrive(&sm.raw_empty[raw_slot]);
     }
-    task = next;
-    next = behind;
-    issue(next);
-    behind = walk();
   }
-  if (!ok) {                                     // no copy is left in flight
-    if (lane == 0) flag_timeout(sm, p);
-    int never = 0;
-    for (; done < issued; ++done) mbar_wait_inline(&sm.raw_full[me][done & 1], (done >> 1) & 1, &never, p.wait_limit);
-  }
+  if (!ok && lane == 0) flag_timeout(sm, p);
 }
 
 template <int D>
@@ -542,6 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_chunk_kernel(cons
   __shared__ Shared sm;
   unsigned char* sQ = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   unsigned char* sKV = sQ + 2 * C::kTileBytes;
+  unsigned char* sRaw = sKV + kSlots * C::kTileBytes;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   if (threadIdx.x == 0) {
     sm.abort_flag = sm.missing = 0;
@@ -552,7 +562,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_chunk_kernel(cons
       mbar_init(&sm.p_full[s][0], 4); mbar_init(&sm.p_full[s][1], 4);
       mbar_init(&sm.o_full[s], 1); mbar_init(&sm.o_free[s], 4);
     }
-    for (int i = 0; i < kWideners; ++i) { mbar_init(&sm.raw_full[i][0], 1); mbar_init(&sm.raw_full[i][1], 1); }
+    for (int i = 0; i < kRaw; ++i) { mbar_init(&sm.raw_full[i], 1); mbar_init(&sm.raw_empty[i], 2); }
     mbar_init(&sm.mma_drain, 1);
     fence_mbar_init();
   }
@@ -573,8 +583,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_chunk_kernel(cons
     } else {
       set_max_registers_down<kRegsOther>();
       if (warp == kWarpMma) mma_role<D>(sm, p, sm.pieces[warp], sQ, sKV, tmem, lane, shares);
-      else widen_role<D>(sm, p, sm.pieces[warp], sKV, sKV + kSlots * C::kTileBytes + (warp - kWarpWiden) * 2 * Unit<D>::kBytes,
-                         warp - kWarpWiden, lane);
+      else if (warp == kWarpLoader) loader_role<D>(sm, p, sm.pieces[warp], sRaw, lane);
+      else widen_role<D>(sm, p, (uint32_t)(shares.begin(blockIdx.x + 1) - shares.begin(blockIdx.x)), sKV, sRaw, warp - kWarpWiden, lane);
     }
   } else if (threadIdx.x == 0) {
     p.records[blockIdx.x] = Record{-1, 0, 0, 0, 0, 0, 0, 0};
