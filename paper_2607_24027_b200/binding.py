@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional
 
@@ -102,6 +103,12 @@ class _CacheArgs(ctypes.Structure):
                 ("stream", ctypes.c_void_p)]
 
 
+# The same layouts for struct.pack, which is several times as fast as building a ctypes structure: a call's host time is what bounds
+# the smallest calls.
+_PACK_CACHE, _PACK_TABLES = struct.Struct("@P6i"), struct.Struct("@10Pq5iP")
+_PACK_NORM, _PACK_ATTENTION = struct.Struct("@4P12q5P9ifP"), struct.Struct("@3P5q3PP6i7ifPNP")
+_PACK_TWO = struct.Struct("@2q")
+
 _lib = None
 
 
@@ -150,17 +157,16 @@ def lib() -> ctypes.CDLL:
                                                                                            ctypes.c_float] + \
                                              [ctypes.c_void_p] * 5
     L.sol_attn_block_tables.restype = ctypes.c_int32
-    L.sol_attn_block_tables.argtypes = [ctypes.POINTER(_TablesArgs)]
+    L.sol_attn_block_tables.argtypes = [ctypes.c_void_p]        # (structures packed by hand)
     L.sol_attn_qk_norm_rope.restype = ctypes.c_int32
-    L.sol_attn_qk_norm_rope.argtypes = [ctypes.POINTER(_NormArgs)]
+    L.sol_attn_qk_norm_rope.argtypes = [ctypes.c_void_p]
     L.sol_attn_cache_bytes.restype = ctypes.c_size_t
     L.sol_attn_cache_bytes.argtypes = [ctypes.c_int] * 4
     for f in (L.sol_attn_cache_append, L.sol_attn_cache_read):
         f.restype = ctypes.c_int32
-        f.argtypes = [ctypes.POINTER(_Cache)] + [ctypes.c_void_p] * 2 + [ctypes.POINTER(ctypes.c_int64)] * 2 + \
-                     [ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_void_p]
+        f.argtypes = [ctypes.c_void_p] * 6 + [ctypes.c_int, ctypes.c_int, ctypes.c_void_p]
     L.sol_attn_cache_attention.restype = ctypes.c_int32
-    L.sol_attn_cache_attention.argtypes = [ctypes.POINTER(_CacheArgs)]
+    L.sol_attn_cache_attention.argtypes = [ctypes.c_void_p]
     L.sol_attn_cache_workspace_bytes.restype = ctypes.c_size_t
     L.sol_attn_cache_workspace_bytes.argtypes = [ctypes.c_int] * 4
     L.sol_attn_cache_read_status.restype = ctypes.c_int32
@@ -180,7 +186,12 @@ def _check(status: int, where: str):
         raise SolAttnError(status, where)
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # 0.1 us; torch.cuda.current_stream() takes 3
+
+
 def _stream(stream: Optional[torch.cuda.Stream]) -> int:
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device())
     s = stream if stream is not None else torch.cuda.current_stream()
     return s.cuda_stream
 
@@ -375,53 +386,60 @@ def sol_attn_debug_set_wait(wait_cycles: int = 0, withhold_tile: int = -1):
 
 
 # ----------------------------------------------------------------------------- cache of keys and values in 4 bits
+# What the library cannot see is checked here: types, shapes, and that everything lies on the current device (a call takes its device and
+# its stream from there).
 _TYPES = {torch.bfloat16: SOL_TYPE_BF16, torch.float16: SOL_TYPE_FP16}
+_I32, _F32, _U8 = torch.int32, torch.float32, torch.uint8
 
 
-def _int32(name, t, *shape, rows_apart=False):
-    """A CUDA int32 tensor of this shape (None: any size); contiguous, or with contiguous rows."""
-    if t.dtype != torch.int32 or not t.is_cuda or t.dim() != len(shape) or any(w is not None and w != h for w, h in zip(shape, t.shape)):
-        raise ValueError(f"{name}: expected a CUDA int32 tensor of shape {list(shape)}")
-    if (t.stride(-1) != 1 and t.shape[-1] > 1) if rows_apart else not t.is_contiguous():
-        raise ValueError(f"{name}: not contiguous")
+def _device(stream) -> int:
+    at = torch.cuda.current_device()
+    if stream is not None and stream.device.index != at:
+        raise ValueError(f"the stream is not one of the current device ({at})")
+    return at
+
+
+def _flat(dev, dtype, name, t, *shape) -> int:
+    """The address of a contiguous tensor of this type and shape on device `dev`; 0 for None."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {list(shape)} on the current CUDA device")
     return t.data_ptr()
 
 
-def _table(t, B):
-    """(pointer, distance of its rows, columns) of a block table of B requests."""
-    at = _int32("block_tables", t, B, None, rows_apart=True)
-    return at, t.stride(0) if B > 1 else t.shape[1], t.shape[1]
+def _table(dev, t, B):
+    """(address, distance of its rows, columns) of a block table of B requests."""
+    if t.dtype is not _I32 or t.get_device() != dev or t.dim() != 2 or t.shape[0] != B or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"block_tables: expected an int32 tensor of {B} contiguous rows on the current CUDA device")
+    columns = t.shape[1]
+    return t.data_ptr(), t.stride(0) if B > 1 else columns, columns
 
 
-def _heads(name, t, dim):
-    """A CUDA bf16 / fp16 tensor of `dim` dimensions whose channels are contiguous."""
-    if t.dim() != dim or t.dtype not in _TYPES or not t.is_cuda or (t.stride(-1) != 1 and t.shape[-1] > 1):
-        raise ValueError(f"{name}: expected a {dim}-dimensional CUDA bf16 or fp16 tensor with contiguous channels")
-    return t
-
-
-def _one_device(stream, *tensors):
-    """The tensors are on the current device, and the stream is one of it (a C call takes both from there)."""
-    at = torch.cuda.current_device()
-    if any(t is not None and t.device.index != at for t in tensors) or (stream is not None and stream.device.index != at):
-        raise ValueError(f"tensors and stream have to be on the current device ({at})")
+def _heads(dev, name, t, shape, dtype):
+    """(address, strides but the last) of a tensor of this shape whose channels are contiguous; a stride of a dimension of one counts as 0."""
+    if t.dtype is not dtype or dtype not in _TYPES or t.get_device() != dev or t.shape != shape:
+        raise ValueError(f"{name}: expected a bf16 or fp16 tensor of shape {list(shape)} on the current CUDA device, of one type with the others")
+    st = t.stride()
+    if st[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"{name}: the channels are not contiguous")
+    if 1 in shape:
+        st = [x if n > 1 else 0 for x, n in zip(st, shape)]
+    return t.data_ptr(), st
 
 
 def sol_attn_block_tables(old_lens, new_lens, free_pages, free_count, block_tables, cu_q, kv_lens, slots, result, page_size,
                           positions=None, stream=None):
     """Pages, slots and positions of this step's tokens: int32 tensors ``old_lens``, ``new_lens``, ``kv_lens`` [requests], ``cu_q``
     [requests + 1], ``block_tables`` [requests, max_blocks], ``slots`` and ``positions`` [max_tokens], ``free_count`` [1], ``result`` [2]."""
-    B = int(old_lens.shape[0])
-    _one_device(stream, old_lens, new_lens, free_pages, free_count, block_tables, cu_q, kv_lens, slots, result, positions)
-    n, (table, table_stride, columns) = int(slots.shape[0]), _table(block_tables, B)
-    a = _TablesArgs(old_lens=_int32("old_lens", old_lens, B), new_lens=_int32("new_lens", new_lens, B),
-                    free_pages=_int32("free_pages", free_pages, None), free_count=_int32("free_count", free_count, 1),
-                    block_tables=table, cu_q=_int32("cu_q", cu_q, B + 1),
-                    kv_lens=_int32("kv_lens", kv_lens, B), slots=_int32("slots", slots, n),
-                    positions=None if positions is None else _int32("positions", positions, n), result=_int32("result", result, 2),
-                    table_stride=table_stride, requests=B, max_blocks=columns, max_tokens=n, free_capacity=int(free_pages.shape[0]),
-                    page_size=int(page_size), stream=_stream(stream))
-    _check(lib().sol_attn_block_tables(ctypes.byref(a)), "sol_attn_block_tables")
+    dev, B, n, free = _device(stream), old_lens.shape[0], slots.shape[0], free_pages.shape[0]
+    table, table_stride, columns = _table(dev, block_tables, B)
+    a = _PACK_TABLES.pack(_flat(dev, _I32, "old_lens", old_lens, B), _flat(dev, _I32, "new_lens", new_lens, B),
+                          _flat(dev, _I32, "free_pages", free_pages, free), _flat(dev, _I32, "free_count", free_count, 1), table,
+                          _flat(dev, _I32, "cu_q", cu_q, B + 1), _flat(dev, _I32, "kv_lens", kv_lens, B), _flat(dev, _I32, "slots", slots, n),
+                          _flat(dev, _I32, "positions", positions, n), _flat(dev, _I32, "result", result, 2), table_stride, B, columns, n, free,
+                          page_size, _stream(stream))
+    _check(lib().sol_attn_block_tables(a), "sol_attn_block_tables")
 
 
 def sol_attn_qk_norm_rope(q, k, q_out, k_out, cos, sin, positions=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False,
@@ -432,31 +450,29 @@ def sol_attn_qk_norm_rope(q, k, q_out, k_out, cos, sin, positions=None, q_weight
     x = q if q is not None else k
     if x is None or (q is None) != (q_out is None) or (k is None) != (k_out is None) or (cos is None) != (sin is None):
         raise ValueError("expected q, k or both, each with its output, and cos with sin")
-    _one_device(stream, q, k, q_out, k_out, cos, sin, positions, q_weight, k_weight)
-    order = (0, 1, 2) if layout == SOL_LAYOUT_BNHD else (0, 2, 1)
-    B, N, d = int(x.shape[0]), int(x.shape[order[1]]), int(x.shape[-1])
-    strides, heads = {}, {}
-    for name, t, other in (("q", q, q_out), ("k", k, k_out), ("q_out", q_out, q), ("k_out", k_out, k)):
-        strides[name], heads[name] = (0, 0, 0), 0
-        if t is not None:
-            _heads(name, t, 4)
-            if t.shape != other.shape or t.dtype != x.dtype or (t.shape[0], t.shape[order[1]], t.shape[3]) != (B, N, d):
-                raise ValueError(f"{name}: shape or type does not match")
-            strides[name] = tuple(t.stride(i) if t.shape[i] > 1 else 0 for i in order)
-            heads[name] = int(t.shape[order[2]])
-    for name, t, shape in (("cos", cos, None), ("sin", sin, None), ("q_weight", q_weight, (d,)), ("k_weight", k_weight, (d,))):
-        if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or (t.dim() != 2 if shape is None else tuple(t.shape) != shape)):
-            raise ValueError(f"{name}: expected a contiguous CUDA fp32 tensor" + (f" of shape {list(shape)}" if shape else " of two dimensions"))
-    if cos is not None and cos.shape != sin.shape:
-        raise ValueError("cos and sin have different shapes")
-    three = ctypes.c_int64 * 3
-    a = _NormArgs(q=_ptr(q), k=_ptr(k), q_out=_ptr(q_out), k_out=_ptr(k_out), q_stride=three(*strides["q"]),
-                  k_stride=three(*strides["k"]), q_out_stride=three(*strides["q_out"]), k_out_stride=three(*strides["k_out"]),
-                  q_weight=_ptr(q_weight), k_weight=_ptr(k_weight), cos=_ptr(cos), sin=_ptr(sin),
-                  positions=None if positions is None else _int32("positions", positions, B, N), batch=B, tokens=N, Hq=heads["q"],
-                  Hk=heads["k"], d=d, rot=0 if cos is None else 2 * int(cos.shape[1]), interleaved=int(interleaved),
-                  table_rows=0 if cos is None else int(cos.shape[0]), type=_TYPES[x.dtype], eps=float(eps), stream=_stream(stream))
-    _check(lib().sol_attn_qk_norm_rope(ctypes.byref(a)), "sol_attn_qk_norm_rope")
+    dev, dtype, shape = _device(stream), x.dtype, tuple(x.shape)
+    if len(shape) != 4:
+        raise ValueError("expected tensors of four dimensions")
+    token, head = (1, 2) if layout == SOL_LAYOUT_BNHD else (2, 1)
+    B, N, d = shape[0], shape[token], shape[3]
+    at, strides, heads = [], [], []
+    for name, a, b in (("q", q, q_out), ("k", k, k_out)):
+        if a is None:
+            at.append((0, 0)), strides.append((0,) * 6), heads.append(0)
+            continue
+        h = a.shape[head] if a.dim() == 4 else 0
+        of = (B, N, h, d) if head == 2 else (B, h, N, d)
+        (pa, sa), (pb, sb) = _heads(dev, name, a, of, dtype), _heads(dev, name + "_out", b, of, dtype)
+        at.append((pa, pb)), heads.append(h)
+        strides.append((sa[0], sa[token], sa[head], sb[0], sb[token], sb[head]))
+    rows, half = (0, 0) if cos is None else cos.shape
+    (q_at, qo_at), (k_at, ko_at) = at
+    (qs, ks) = strides
+    a = _PACK_NORM.pack(q_at, k_at, qo_at, ko_at, *qs[:3], *ks[:3], *qs[3:], *ks[3:], _flat(dev, _F32, "q_weight", q_weight, d),
+                        _flat(dev, _F32, "k_weight", k_weight, d), _flat(dev, _F32, "cos", cos, rows, half),
+                        _flat(dev, _F32, "sin", sin, rows, half), _flat(dev, _I32, "positions", positions, B, N), B, N, *heads, d, 2 * half,
+                        bool(interleaved), rows, _TYPES[dtype], eps, _stream(stream))
+    _check(lib().sol_attn_qk_norm_rope(a), "sol_attn_qk_norm_rope")
 
 
 @dataclass
@@ -470,11 +486,17 @@ class Cache:
     k_exp: int = 0
     v_exp: int = 0
 
-    def c(self) -> _Cache:
-        need = sol_attn_cache_bytes(self.pages, self.page_size, self.heads, self.d)
-        if self.data.dtype != torch.uint8 or not self.data.is_cuda or not self.data.is_contiguous() or self.data.numel() < need:
-            raise ValueError(f"cache: expected a contiguous CUDA uint8 tensor of {need} bytes")
-        return _Cache(self.data.data_ptr(), self.pages, self.page_size, self.heads, self.d, self.k_exp, self.v_exp)
+    def __post_init__(self):
+        self.bytes = sol_attn_cache_bytes(self.pages, self.page_size, self.heads, self.d)
+        if self.bytes == 0:
+            raise SolAttnError(SOL_ERR_UNSUPPORTED_SHAPE, "sol_attn_cache_bytes")
+
+    def c(self, dev: int):
+        """The members of ``sol_attn_cache``."""
+        t = self.data
+        if t.dtype is not _U8 or t.get_device() != dev or not t.is_contiguous() or t.numel() < self.bytes:
+            raise ValueError(f"cache: expected a contiguous uint8 tensor of {self.bytes} bytes on the current CUDA device")
+        return t.data_ptr(), self.pages, self.page_size, self.heads, self.d, self.k_exp, self.v_exp
 
 
 def sol_attn_cache_bytes(pages, page_size, heads, d) -> int:
@@ -484,22 +506,18 @@ def sol_attn_cache_bytes(pages, page_size, heads, d) -> int:
 def make_cache(pages, page_size, heads, d, k_exp=0, v_exp=0, device="cuda") -> Cache:
     """Allocate (with torch) an empty cache."""
     n = sol_attn_cache_bytes(pages, page_size, heads, d)
-    if n == 0:
-        raise SolAttnError(SOL_ERR_UNSUPPORTED_SHAPE, "sol_attn_cache_bytes")
     return Cache(torch.zeros(n, dtype=torch.uint8, device=device), pages, page_size, heads, d, k_exp, v_exp)
 
 
 def _cache_rows(cache, k, v, slots, stream):
-    _one_device(stream, cache.data, k, v, slots)
-    x = k if k is not None else v
+    dev, x, n = _device(stream), k if k is not None else v, slots.shape[0]
     if x is None:
         raise ValueError("expected k, v or both")
-    n, strides = int(slots.shape[0]), []
-    for name, t in (("k", k), ("v", v)):
-        if t is not None and (_heads(name, t, 3).dtype != x.dtype or tuple(t.shape) != (n, cache.heads, cache.d)):
-            raise ValueError(f"{name}: expected shape {[n, cache.heads, cache.d]}, k and v of one type")
-        strides.append((ctypes.c_int64 * 2)(*((0, 0) if t is None else (t.stride(i) if t.shape[i] > 1 else 0 for i in (0, 1)))))
-    return ctypes.byref(cache.c()), _ptr(k), _ptr(v), *strides, _int32("slots", slots, n), n, _TYPES[x.dtype], _stream(stream)
+    shape, dtype = (n, cache.heads, cache.d), x.dtype
+    k_at, ks = (0, (0, 0)) if k is None else _heads(dev, "k", k, shape, dtype)
+    v_at, vs = (0, (0, 0)) if v is None else _heads(dev, "v", v, shape, dtype)
+    return (_PACK_CACHE.pack(*cache.c(dev)), k_at, v_at, _PACK_TWO.pack(ks[0], ks[1]), _PACK_TWO.pack(vs[0], vs[1]),
+            _flat(dev, _I32, "slots", slots, n), n, _TYPES[dtype], _stream(stream))
 
 
 def sol_attn_cache_append(k, v, slots, cache: Cache, stream=None):
@@ -532,24 +550,18 @@ def sol_attn_cache_attention(q, cu_q, kv_lens, block_tables, cache: Cache, out, 
                              stream=None):
     """Attention of ``q`` [tokens, heads, d] (request b: rows cu_q[b] to cu_q[b + 1]) over the first kv_lens[b] tokens of each
     request's pages, into ``out`` (as q) and ``lse`` (fp32 [tokens, heads])."""
-    _one_device(stream, q, cu_q, kv_lens, block_tables, cache.data, out, workspace, lse)
-    _heads("q", q, 3), _heads("out", out, 3)
-    n, H, d = (int(x) for x in q.shape)
-    if out.shape != q.shape or out.dtype != q.dtype or d != cache.d:
-        raise ValueError("q and out have to agree in shape and type, and with the cache in d")
-    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or tuple(lse.shape) != (n, H)):
-        raise ValueError("lse: expected a contiguous CUDA fp32 tensor of shape [tokens, heads]")
-    if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
-        raise ValueError("workspace: expected a contiguous CUDA uint8 tensor")
-    B, two = int(kv_lens.shape[0]), ctypes.c_int64 * 2
-    table, table_stride, columns = _table(block_tables, B)
-    a = _CacheArgs(q=_ptr(q), out=_ptr(out), lse=_ptr(lse), q_stride=two(*(q.stride(i) if q.shape[i] > 1 else 0 for i in (0, 1))),
-                   out_stride=two(*(out.stride(i) if out.shape[i] > 1 else 0 for i in (0, 1))),
-                   table_stride=table_stride, cu_q=_int32("cu_q", cu_q, B + 1), kv_lens=_int32("kv_lens", kv_lens, B), block_tables=table,
-                   cache=cache.c(), tokens=n, requests=B, max_blocks=columns, max_q=int(max_q), Hq=H,
-                   type=_TYPES[q.dtype], causal=int(causal), scale=float(scale), workspace=workspace.data_ptr(),
-                   workspace_bytes=workspace.numel(), stream=_stream(stream))
-    _check(lib().sol_attn_cache_attention(ctypes.byref(a)), "sol_attn_cache_attention")
+    dev, shape, dtype, B = _device(stream), tuple(q.shape), q.dtype, kv_lens.shape[0]
+    if len(shape) != 3 or shape[2] != cache.d:
+        raise ValueError("expected q of three dimensions, and the cache's d")
+    (q_at, qs), (o_at, os_) = _heads(dev, "q", q, shape, dtype), _heads(dev, "out", out, shape, dtype)
+    table, table_stride, columns = _table(dev, block_tables, B)
+    if workspace.dtype is not _U8 or workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace: expected a contiguous uint8 tensor on the current CUDA device")
+    a = _PACK_ATTENTION.pack(q_at, o_at, _flat(dev, _F32, "lse", lse, *shape[:2]), qs[0], qs[1], os_[0], os_[1], table_stride,
+                             _flat(dev, _I32, "cu_q", cu_q, B + 1), _flat(dev, _I32, "kv_lens", kv_lens, B), table, *cache.c(dev), shape[0], B,
+                             columns, max_q, shape[1], _TYPES[dtype], bool(causal), scale, workspace.data_ptr(), workspace.numel(),
+                             _stream(stream))
+    _check(lib().sol_attn_cache_attention(a), "sol_attn_cache_attention")
 
 
 def sol_attn_cache_read_status(workspace, stream=None) -> int:

@@ -143,14 +143,47 @@ def test_bad_tables_are_refused(sb, change, why):
     assert sb.lib().sol_attn_block_tables(None) == sb.SOL_ERR_INVALID_ARG
 
 
+def test_packed_structures_match_the_header_s(sb):
+    """The bytes that the binding packs are the C structures: sizes, and every field where it belongs."""
+    for cls, pack in ((sb._Cache, sb._PACK_CACHE), (sb._TablesArgs, sb._PACK_TABLES), (sb._NormArgs, sb._PACK_NORM),
+                      (sb._CacheArgs, sb._PACK_ATTENTION)):
+        assert ctypes.sizeof(cls) == pack.size, cls
+
+        def leaves(c):
+            for name, t in c._fields_:
+                if isinstance(t, type) and issubclass(t, ctypes.Structure):
+                    yield from leaves(t)
+                elif isinstance(t, type) and issubclass(t, ctypes.Array):
+                    yield from ((t._type_, x) for x in range(t._length_))
+                else:
+                    yield t, 0
+
+        def values(obj):
+            for name, t in obj._fields_:
+                v = getattr(obj, name)
+                if isinstance(v, ctypes.Structure):
+                    yield from values(v)
+                elif isinstance(v, ctypes.Array):
+                    yield from v
+                else:
+                    yield v
+
+        n = len(list(leaves(cls)))
+        obj = cls.from_buffer_copy(pack.pack(*range(1, n + 1)))
+        assert list(values(obj)) == list(range(1, n + 1)), cls
+
+
 def test_binding_refuses_what_the_kernels_could_not_know(sb):
     cache = sb.Cache(torch.zeros(10, dtype=torch.uint8), 4, 16, 2, 128)
     with pytest.raises(ValueError):
-        cache.c()
+        cache.c(0)
+    with pytest.raises(sb.SolAttnError):
+        sb.Cache(torch.zeros(10, dtype=torch.uint8), 4, 24, 2, 128)
     with pytest.raises(ValueError):
-        sb._int32("x", torch.zeros(3, dtype=torch.int32), 3)                    # not on a GPU
+        sb._flat(0, torch.int32, "x", torch.zeros(3, dtype=torch.int32), 3)     # not on a GPU
     with pytest.raises(ValueError):
-        sb._heads("x", torch.zeros(3, 2, 64), 3)                                # not a 16-bit type
+        sb._heads(-1, "x", torch.zeros(3, 2, 64), (3, 2, 64), torch.float32)    # not a 16-bit type
+    assert sb._flat(0, torch.int32, "x", None, 3) == 0
 
 
 @pytest.mark.parametrize("value, code", [(0.25, 0), (0.26, 1), (0.75, 2), (0.74, 1), (1.25, 2), (1.75, 4), (2.5, 4), (3.5, 6), (5.0, 6), (5.1, 7)])

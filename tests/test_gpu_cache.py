@@ -479,6 +479,8 @@ def test_refusals_of_the_binding(sb):
         sb.sol_attn_cache_append(q, q, ints([1, 2]), cache)               # four heads into a cache of two
     with pytest.raises(ValueError):
         sb.sol_attn_qk_norm_rope(q[None], None, None, None, None, None)
+    with pytest.raises(ValueError):
+        sb.sol_attn_qk_norm_rope(q[None], q[None].half(), q[None], q[None].half(), None, None)
     with pytest.raises(sb.SolAttnError):
         x = torch.zeros(1, 2, 4, 72, dtype=torch.bfloat16, device="cuda")
         sb.sol_attn_qk_norm_rope(x, None, x, None, None, None)
