@@ -45,6 +45,11 @@ inline sol_status_t check(const sol_attn_cache* c) {
   return sol_attn_cache_bytes(c->pages, c->page_size, c->Hk, c->d) ? SOL_OK : SOL_ERR_UNSUPPORTED_SHAPE;
 }
 
+inline int page_shift(int page_size) {           // of a supported size
+  int s = 4;
+  while (1 << s < page_size) ++s;
+  return s;
+}
 inline bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 inline bool strides_ok(const int64_t* s, int n) {
   for (int i = 0; i < n; ++i)
@@ -55,14 +60,15 @@ inline bool strides_ok(const int64_t* s, int n) {
 #ifdef __CUDACC__
 // Where a slot's unit of a head starts.
 template <int D>
-__device__ __forceinline__ size_t unit_at(int slot, int head, int page_size, int heads) {
-  const int page = slot / page_size, unit = (slot - page * page_size) / kUnit;
-  return (((size_t)page * heads + head) * (page_size / kUnit) + unit) * Unit<D>::kBytes;
+__device__ __forceinline__ size_t unit_at(int slot, int head, int page_shift, int heads) {
+  const int page = slot >> page_shift, unit = (slot & ((1 << page_shift) - 1)) / kUnit;
+  return (((size_t)((long long)page * heads + head) << (page_shift - 4)) + unit) * Unit<D>::kBytes;
 }
 
 // 16-bit types by name.
 template <class T> struct Two;
 template <> struct Two<__nv_bfloat16> {
+  static constexpr uint32_t kInf = 0x7f80;       // bits of infinity
   __device__ static float2 widen(uint32_t x) { return __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&x)); }
   __device__ static uint32_t round(float a, float b) {
     const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
@@ -70,6 +76,7 @@ template <> struct Two<__nv_bfloat16> {
   }
 };
 template <> struct Two<__half> {
+  static constexpr uint32_t kInf = 0x7c00;
   __device__ static float2 widen(uint32_t x) { return __half22float2(*reinterpret_cast<__half2*>(&x)); }
   __device__ static uint32_t round(float a, float b) {
     const __half2 r = __floats2half2_rn(a, b);

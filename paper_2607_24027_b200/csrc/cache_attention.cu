@@ -656,7 +656,7 @@ sol_status_t sol_attn_cache_attention(const sol_attn_cache_args* a) {
   p.data = static_cast<const unsigned char*>(a->cache.data);
   p.tokens = a->tokens; p.requests = a->requests; p.max_blocks = a->max_blocks;
   p.Hq = a->Hq; p.Hk = a->cache.Hk; p.group = a->Hq / a->cache.Hk; p.causal = a->causal != 0; p.pages = a->cache.pages;
-  p.page_shift = a->cache.page_size == 16 ? 4 : a->cache.page_size == 32 ? 5 : a->cache.page_size == 64 ? 6 : a->cache.page_size == 128 ? 7 : 8;
+  p.page_shift = cache::page_shift(a->cache.page_size);
   const float scale = a->scale > 0.f ? a->scale : 1.0f / std::sqrt((float)a->cache.d);
   p.sl2 = std::ldexp(scale * 1.4426950408889634f, a->cache.k_exp);
   p.v_scale = std::ldexp(1.0f, a->cache.v_exp);

@@ -14,24 +14,23 @@ struct WriteParams {
   long long k_s[2], v_s[2];
   const int32_t* slots;
   unsigned char* data;
-  long long rows;                                // tokens * Hk
-  int Hk, page_size, slot_end, k_exp, v_exp;
+  uint32_t rows;                                 // tokens * Hk
+  int Hk, page_shift, slot_end, k_exp, v_exp;
 };
 
 // Which row, group and side of a row (key or value) a thread has.
 template <int D>
 struct Place {
-  long long row;
+  uint32_t row;
   int group, token, head;
   bool is_value;
   __device__ Place(const WriteParams& p) {
     constexpr int kGroups = D / 16;
-    const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
-    group = (int)(i % kGroups);
-    is_value = (i / kGroups) % 2;
-    row = i / (2 * kGroups);
-    token = (int)(row / p.Hk);
-    head = (int)(row - (long long)token * p.Hk);
+    group = threadIdx.x % kGroups;
+    is_value = (threadIdx.x / kGroups) % 2;
+    row = blockIdx.x * (kThreads / (2 * kGroups)) + threadIdx.x / (2 * kGroups);
+    token = (int)(row / (uint32_t)p.Hk);
+    head = (int)(row - (uint32_t)token * p.Hk);
   }
 };
 
@@ -45,49 +44,55 @@ __global__ void __launch_bounds__(kThreads) cache_append_kernel(const WriteParam
   const bool on = at.row < p.rows;
   const int slot = on ? p.slots[at.token] : -1;
   const bool stored = slot >= 0 && slot < p.slot_end;
-  float x[16];
-  bool bad = false;
-  float most = 0.f;
-  const float unscale = cache::power2(-(at.is_value ? p.v_exp : p.k_exp));
+  uint32_t w[8];
+  uint32_t most2 = 0;                            // the largest |x| of either half of the words: 16-bit floats are in the order of their bits
   if (stored) {
     const T* src = at.is_value ? (const T*)p.v + at.token * p.v_s[0] + at.head * p.v_s[1]
                                : (const T*)p.k + at.token * p.k_s[0] + at.head * p.k_s[1];
     const uint4* in = reinterpret_cast<const uint4*>(src + at.group * 16);
     const uint4 a = in[0], b = in[1];
-    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { const float2 f = Two<T>::widen(w[i]); x[2 * i] = f.x; x[2 * i + 1] = f.y; }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if (!isfinite(x[i])) { bad = true; x[i] = 0.f; }
-      x[i] *= unscale;
-      most = fmaxf(most, fabsf(x[i]));
-    }
+    for (int i = 0; i < 8; ++i) most2 = __vmaxu2(most2, w[i] & 0x7fff7fffu);
   }
+  uint32_t most16 = max(most2 & 0xffffu, most2 >> 16);
   // one element that is not finite marks its token's key
+  const bool bad = most16 >= Two<T>::kInf;
   const unsigned mine = ((1u << (2 * kGroups)) - 1u) << ((threadIdx.x % 32) / (2 * kGroups) * (2 * kGroups));
   const bool mark = (__ballot_sync(0xffffffffu, bad) & mine) != 0;
   if (!stored) return;
+  if (bad) {                                     // such elements count as zero
+    most16 = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if ((w[i] & 0x7fffu) >= Two<T>::kInf) w[i] &= 0xffff0000u;
+      if ((w[i] >> 16 & 0x7fffu) >= Two<T>::kInf) w[i] &= 0xffffu;
+      most16 = max(most16, max(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
+    }
+  }
+  const float unscale = cache::power2(-(at.is_value ? p.v_exp : p.k_exp)), most = Two<T>::widen(most16).x * unscale;
   // max|x| has at most 11 significant bits and a tie of e4m3 times 6 has 7, so the quotient, rounded to fp32, is a tie only if it is one.
   const __nv_fp8_storage_t s8 = __nv_cvt_float_to_fp8(fminf(__fdiv_rn(most, 6.f), 448.f), __NV_SATFINITE, __NV_E4M3);
   const float s = __half2float(__half(__nv_cvt_fp8_to_halfraw(s8, __NV_E4M3)));
-  const float inv = s > 0.f ? 1.f / s : 0.f;
+  // x 2^-exp / s by the reciprocal is off by 2^-23 at most, which would break ties (0.75 s and the like).  A quotient that is no
+  // tie is 2^-11 or more away from one (x has 11 bits at most, s times a tie 7), so rounding to 12 bits (Veltkamp's
+  // splitting) puts ties back in place and moves nothing across one.
+  const float inv = s > 0.f ? unscale / s : 0.f;
+  const bool over = most > 6.5f * 448.f;         // only then a quotient may pass 7, and much further
+  const float2 inv2 = make_float2(inv, inv), split2 = make_float2(4097.f, 4097.f), zero2 = make_float2(0.f, 0.f),
+               minus2 = make_float2(-1.f, -1.f);
   unsigned long long codes = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    float2 t;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      // x / s by the reciprocal is off by 2^-23 at most, which would break ties (0.75 s and the like).  A quotient that is no
-      // tie is 2^-11 or more away from one (x has 11 bits at most, s times a tie 7), so rounding to 12 bits (Veltkamp's
-      // splitting) puts ties back in place and moves nothing across one.
-      const float y = fminf(fmaxf(x[2 * i + j] * inv, -8.f), 8.f);
-      const float c = __fmul_rn(y, 4097.f);
-      (j ? t.y : t.x) = __fsub_rn(c, __fsub_rn(c, y));
+    float2 y = __ffma2_rn(Two<T>::widen(w[i]), inv2, zero2);
+    if (over) {
+      y.x = fminf(fmaxf(y.x, -8.f), 8.f);
+      y.y = fminf(fmaxf(y.y, -8.f), 8.f);
     }
+    const float2 c = __ffma2_rn(y, split2, zero2), t = __ffma2_rn(__ffma2_rn(y, minus2, c), minus2, c);
     codes |= (unsigned long long)__nv_cvt_float2_to_fp4x2(t, __NV_E2M1, cudaRoundNearest) << (8 * i);
   }
-  unsigned char* unit = p.data + cache::unit_at<D>(slot, at.head, p.page_size, p.Hk);
+  unsigned char* unit = p.data + cache::unit_at<D>(slot, at.head, p.page_shift, p.Hk);
   const int i = slot % cache::kUnit;
   if (at.is_value) {
     unsigned char* dst = unit + U::value_codes(i, at.group);
@@ -114,7 +119,7 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const WriteParams 
   T* dst = (T*)const_cast<void*>(at.is_value ? p.v : p.k);
   const int slot = p.slots[at.token];
   if (!dst || slot < 0 || slot >= p.slot_end) return;
-  const unsigned char* unit = p.data + cache::unit_at<D>(slot, at.head, p.page_size, p.Hk);
+  const unsigned char* unit = p.data + cache::unit_at<D>(slot, at.head, p.page_shift, p.Hk);
   const int i = slot % cache::kUnit;
   unsigned long long codes;
   uint32_t s8;
@@ -165,13 +170,13 @@ sol_status_t launch(int what, const sol_attn_cache* c, const void* k, const void
   for (int i = 0; i < 2; ++i) { p.k_s[i] = k ? ks[i] : 0; p.v_s[i] = v ? vs[i] : 0; }
   p.slots = slots;
   p.data = static_cast<unsigned char*>(c->data);
-  p.rows = (long long)tokens * c->Hk;
-  p.Hk = c->Hk; p.page_size = c->page_size; p.slot_end = c->pages * c->page_size;
+  if ((long long)tokens * c->Hk > 0x7fffffffLL) return SOL_ERR_UNSUPPORTED_SHAPE;
+  p.rows = (uint32_t)tokens * (uint32_t)c->Hk;
+  p.Hk = c->Hk; p.page_shift = cache::page_shift(c->page_size); p.slot_end = c->pages * c->page_size;
   p.k_exp = c->k_exp; p.v_exp = c->v_exp;
-  const long long blocks = (p.rows * (2 * c->d / 16) + kThreads - 1) / kThreads;
-  if (blocks > 0x7fffffffLL) return SOL_ERR_UNSUPPORTED_SHAPE;
+  const uint32_t per_block = kThreads / (2 * c->d / 16), blocks = (p.rows + per_block - 1) / per_block;
   auto run = [&](auto kernel) {
-    return launch_after(kernel, dim3((unsigned)blocks), kThreads, 0, 0, 0, static_cast<cudaStream_t>(stream), p);
+    return launch_after(kernel, dim3(blocks), kThreads, 0, 0, 0, static_cast<cudaStream_t>(stream), p);
   };
   cudaError_t e;
   if (what == kAppend)

@@ -2,7 +2,8 @@
 //
 // Bound by HBM: every element is read and written once.  A lane holds 8 channels (16 bytes) of a head, so d / 8 lanes hold a
 // head and a warp 2 (d = 128) or 4 (d = 64) heads at a time; the partner channels of a pair are in the same lane, or rot / 16
-// lanes further.  A warp keeps to one token, whose cos and sin it reads once for all of its heads.
+// lanes further.  A warp keeps to one token, whose cos and sin it reads once for all of its heads.  (Next to HBM comes issuing the
+// instructions: pairs of fp32 numbers go by one, and partners change places as 16-bit pairs.)
 #include "cache.cuh"
 
 namespace sol {
@@ -33,7 +34,8 @@ __global__ void __launch_bounds__(kWarps * 32) qk_norm_rope_kernel(const NormPar
   const int pos = p.positions ? p.positions[token] : n;
   if (p.rot > 0 && (pos < 0 || pos >= p.table_rows)) return;
   const int half = p.rot / 2;
-  // cos and sin of this lane's pairs: 8 (partner in another lane), or 4 (both here)
+  // Pairs: the lane's channel i and its partner, i ^ 1 of the lane (interleaved), or channel i of lane `partner`.  With the norm r, weights w
+  // and the partner's weights u, the result is r (x w cos +- y u sin): two factors per channel, formed once for all heads.
   const bool turns = c0 < p.rot, upper = !p.interleaved && c0 >= half;
   const int partner = p.interleaved || !turns ? lane : lane + (upper ? -half : half) / 8;
   float cs[8], sn[8];
@@ -41,68 +43,72 @@ __global__ void __launch_bounds__(kWarps * 32) qk_norm_rope_kernel(const NormPar
   for (int i = 0; i < 8; ++i) { cs[i] = 1.f; sn[i] = 0.f; }
   if (turns) {
     const size_t at = (size_t)pos * half + (p.interleaved ? c0 / 2 : (upper ? c0 - half : c0));
-#pragma unroll
-    for (int i = 0; i < 8; i += 4) {
-      if (i == 0 || !p.interleaved) {
-        const float4 x = __ldg(reinterpret_cast<const float4*>(p.cos + at + i)), y = __ldg(reinterpret_cast<const float4*>(p.sin + at + i));
-        cs[i] = x.x; cs[i + 1] = x.y; cs[i + 2] = x.z; cs[i + 3] = x.w;
-        sn[i] = y.x; sn[i + 1] = y.y; sn[i + 2] = y.z; sn[i + 3] = y.w;
-      }
+    const float4 x = __ldg(reinterpret_cast<const float4*>(p.cos + at)), y = __ldg(reinterpret_cast<const float4*>(p.sin + at));
+    if (p.interleaved) {
+      cs[0] = cs[1] = x.x; cs[2] = cs[3] = x.y; cs[4] = cs[5] = x.z; cs[6] = cs[7] = x.w;
+      sn[0] = -y.x; sn[1] = y.x; sn[2] = -y.y; sn[3] = y.y; sn[4] = -y.z; sn[5] = y.z; sn[6] = -y.w; sn[7] = y.w;
+    } else {
+      const float4 x1 = __ldg(reinterpret_cast<const float4*>(p.cos + at + 4)), y1 = __ldg(reinterpret_cast<const float4*>(p.sin + at + 4));
+      const float f = upper ? 1.f : -1.f;
+      cs[0] = x.x; cs[1] = x.y; cs[2] = x.z; cs[3] = x.w; cs[4] = x1.x; cs[5] = x1.y; cs[6] = x1.z; cs[7] = x1.w;
+      sn[0] = f * y.x; sn[1] = f * y.y; sn[2] = f * y.z; sn[3] = f * y.w; sn[4] = f * y1.x; sn[5] = f * y1.y; sn[6] = f * y1.z; sn[7] = f * y1.w;
     }
   }
-  const int h_end = min(p.heads, ((int)blockIdx.y + 1) * p.per_warp);
-  for (int h0 = blockIdx.y * p.per_warp; h0 < h_end; h0 += kRows * kInFlight) {
-    uint4 raw[kInFlight];
-#pragma unroll
-    for (int u = 0; u < kInFlight; ++u) {
-      const int h = h0 + u * kRows + sub;
-      raw[u] = make_uint4(0, 0, 0, 0);
-      if (h < h_end) {
-        const T* src = h < p.Hq ? (const T*)p.q + b * p.q_s[0] + n * p.q_s[1] + h * p.q_s[2]
-                                : (const T*)p.k + b * p.k_s[0] + n * p.k_s[1] + (h - p.Hq) * p.k_s[2];
-        raw[u] = *reinterpret_cast<const uint4*>(src + c0);
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < kInFlight; ++u) {
-      const int h = h0 + u * kRows + sub;
-      if (h0 + u * kRows >= h_end) break;        // (the whole warp)
-      const bool is_q = h < p.Hq;
-      const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
-      float x[8];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) { const float2 f = Two<T>::widen(w[i]); x[2 * i] = f.x; x[2 * i + 1] = f.y; }
-      float sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
-#pragma unroll
-      for (int o = 1; o < kLanes; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      const float r = rsqrtf(sum * (1.f / D) + p.eps);
-      const float* weight = is_q ? p.q_weight : p.k_weight;
+  const int h_begin = blockIdx.y * p.per_warp, h_end = min(p.heads, h_begin + p.per_warp);
+#pragma unroll 1
+  for (int side = 0; side < 2; ++side) {         // q, then k
+    const int first = side ? max(h_begin, p.Hq) - p.Hq : h_begin, end = side ? h_end - p.Hq : min(h_end, p.Hq);
+    if (first >= end) continue;
+    const float* weight = side ? p.k_weight : p.q_weight;
+    const T* src = (side ? (const T*)p.k + b * p.k_s[0] + n * p.k_s[1] : (const T*)p.q + b * p.q_s[0] + n * p.q_s[1]) + c0;
+    T* dst = (side ? (T*)p.k_out + b * p.ko_s[0] + n * p.ko_s[1] : (T*)p.q_out + b * p.qo_s[0] + n * p.qo_s[1]) + c0;
+    const long long from = side ? p.k_s[2] : p.q_s[2], to = side ? p.ko_s[2] : p.qo_s[2];
+    float2 own[4], other[4];
+    {
+      float w[8], u[8];
 #pragma unroll
       for (int i = 0; i < 8; i += 4) {
         const float4 g = weight ? __ldg(reinterpret_cast<const float4*>(weight + c0 + i)) : make_float4(1.f, 1.f, 1.f, 1.f);
-        x[i] *= r * g.x; x[i + 1] *= r * g.y; x[i + 2] *= r * g.z; x[i + 3] *= r * g.w;
+        w[i] = g.x; w[i + 1] = g.y; w[i + 2] = g.z; w[i + 3] = g.w;
       }
-      if (p.interleaved) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) u[i] = p.interleaved ? w[i ^ 1] : __shfl_sync(0xffffffffu, w[i], partner);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        own[i] = make_float2(w[2 * i] * cs[2 * i], w[2 * i + 1] * cs[2 * i + 1]);
+        other[i] = make_float2(u[2 * i] * sn[2 * i], u[2 * i + 1] * sn[2 * i + 1]);
+      }
+    }
+#pragma unroll 1
+    for (int h0 = first; h0 < end; h0 += kRows * kInFlight) {
+      uint4 raw[kInFlight];
+#pragma unroll
+      for (int v = 0; v < kInFlight; ++v) {
+        const int h = h0 + v * kRows + sub;
+        raw[v] = make_uint4(0, 0, 0, 0);
+        if (h < end) raw[v] = *reinterpret_cast<const uint4*>(src + h * from);
+      }
+#pragma unroll
+      for (int v = 0; v < kInFlight; ++v) {
+        const int h = h0 + v * kRows + sub;
+        if (h0 + v * kRows >= end) break;        // (the whole warp)
+        const uint32_t w[4] = {raw[v].x, raw[v].y, raw[v].z, raw[v].w};
+        float2 x[4], sum2 = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { x[i] = Two<T>::widen(w[i]); sum2 = __ffma2_rn(x[i], x[i], sum2); }
+        float sum = sum2.x + sum2.y;
+#pragma unroll
+        for (int o = 1; o < kLanes; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        const float r = rsqrtf(sum * (1.f / D) + p.eps);
+        const float2 r2 = make_float2(r, r);
+        uint32_t out[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float a = x[2 * i], c = x[2 * i + 1];
-          x[2 * i] = a * cs[i] - c * sn[i];
-          x[2 * i + 1] = a * sn[i] + c * cs[i];
+          const float2 y = p.interleaved ? make_float2(x[i].y, x[i].x) : Two<T>::widen(__shfl_sync(0xffffffffu, w[i], partner));
+          const float2 z = __ffma2_rn(__ffma2_rn(y, other[i], __ffma2_rn(x[i], own[i], make_float2(0.f, 0.f))), r2, make_float2(0.f, 0.f));
+          out[i] = Two<T>::round(z.x, z.y);
         }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {            // (lanes that do not turn get their own value and sin 0)
-          const float y = __shfl_sync(0xffffffffu, x[i], partner);
-          x[i] = x[i] * cs[i] + (upper ? y : -y) * sn[i];
-        }
-      }
-      if (h < h_end) {
-        T* dst = is_q ? (T*)p.q_out + b * p.qo_s[0] + n * p.qo_s[1] + h * p.qo_s[2]
-                      : (T*)p.k_out + b * p.ko_s[0] + n * p.ko_s[1] + (h - p.Hq) * p.ko_s[2];
-        *reinterpret_cast<uint4*>(dst + c0) = make_uint4(Two<T>::round(x[0], x[1]), Two<T>::round(x[2], x[3]),
-                                                         Two<T>::round(x[4], x[5]), Two<T>::round(x[6], x[7]));
+        if (h < end) *reinterpret_cast<uint4*>(dst + h * to) = make_uint4(out[0], out[1], out[2], out[3]);
       }
     }
   }
