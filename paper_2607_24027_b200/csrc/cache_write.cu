@@ -1,11 +1,14 @@
 // Keys and values into the 4-bit cache and back (sol_attn_cache_append, sol_attn_cache_read).
 //
-// Bound by HBM: 4 d bytes of a token and head on one side, 9 d / 8 on the other.  A lane has one group of 16 channels of one
-// token; d / 16 lanes have a key, the next d / 16 the value, so a warp has 2 (d = 128) or 4 (d = 64) rows of a key and a value.
+// Bound by HBM: 4 d bytes of a token and head on one side, 9 d / 8 on the other; and next to that by issuing the instructions, of which
+// finding the place takes as many as 16 channels do.  So a lane has 32 channels of one token, two groups; d / 32 lanes have a key,
+// the next d / 32 the value.
 #include "cache.cuh"
 
 namespace sol {
 namespace {
+
+using cache::Two;
 
 constexpr int kThreads = 128;
 
@@ -18,101 +21,133 @@ struct WriteParams {
   int Hk, page_shift, slot_end, k_exp, v_exp;
 };
 
-// Which row, group and side of a row (key or value) a thread has.
+// Which row, part of 32 channels and side of a row (key or value) a thread has.
 template <int D>
 struct Place {
+  static constexpr int kParts = D / 32;
   uint32_t row;
-  int group, token, head;
+  int part, token, head;
   bool is_value;
   __device__ Place(const WriteParams& p) {
-    constexpr int kGroups = D / 16;
-    group = threadIdx.x % kGroups;
-    is_value = (threadIdx.x / kGroups) % 2;
-    row = blockIdx.x * (kThreads / (2 * kGroups)) + threadIdx.x / (2 * kGroups);
+    part = threadIdx.x % kParts;
+    is_value = (threadIdx.x / kParts) % 2;
+    row = blockIdx.x * (kThreads / (2 * kParts)) + threadIdx.x / (2 * kParts);
     token = (int)(row / (uint32_t)p.Hk);
     head = (int)(row - (uint32_t)token * p.Hk);
   }
 };
 
-template <class T, int D>
-__global__ void __launch_bounds__(kThreads) cache_append_kernel(const WriteParams p) {
-  using U = cache::Unit<D>;
-  using cache::Two;
-  constexpr int kGroups = D / 16;
-  const Place<D> at(p);
-  kernel_wait();
-  const bool on = at.row < p.rows;
-  const int slot = on ? p.slots[at.token] : -1;
-  const bool stored = slot >= 0 && slot < p.slot_end;
-  uint32_t w[8];
-  uint32_t most2 = 0;                            // the largest |x| of either half of the words: 16-bit floats are in the order of their bits
-  if (stored) {
-    const T* src = at.is_value ? (const T*)p.v + at.token * p.v_s[0] + at.head * p.v_s[1]
-                               : (const T*)p.k + at.token * p.k_s[0] + at.head * p.k_s[1];
-    const uint4* in = reinterpret_cast<const uint4*>(src + at.group * 16);
-    const uint4 a = in[0], b = in[1];
-    w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) most2 = __vmaxu2(most2, w[i] & 0x7fff7fffu);
-  }
-  uint32_t most16 = max(most2 & 0xffffu, most2 >> 16);
-  // one element that is not finite marks its token's key
-  const bool bad = most16 >= Two<T>::kInf;
-  const unsigned mine = ((1u << (2 * kGroups)) - 1u) << ((threadIdx.x % 32) / (2 * kGroups) * (2 * kGroups));
-  const bool mark = (__ballot_sync(0xffffffffu, bad) & mine) != 0;
-  if (!stored) return;
-  if (bad) {                                     // such elements count as zero
-    most16 = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if ((w[i] & 0x7fffu) >= Two<T>::kInf) w[i] &= 0xffff0000u;
-      if ((w[i] >> 16 & 0x7fffu) >= Two<T>::kInf) w[i] &= 0xffffu;
-      most16 = max(most16, max(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
-    }
-  }
-  const float unscale = cache::power2(-(at.is_value ? p.v_exp : p.k_exp)), most = Two<T>::widen(most16).x * unscale;
+// Four e2m1 pairs to a word, the first number of each in the lower four bits.
+__device__ __forceinline__ uint32_t pack_codes(const float2 (&x)[4]) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\tcvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\tmov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(r)
+      : "f"(x[0].x), "f"(x[0].y), "f"(x[1].x), "f"(x[1].y), "f"(x[2].x), "f"(x[2].y), "f"(x[3].x), "f"(x[3].y));
+  return r;
+}
+
+// Codes of 16 channels in eight words of 16-bit numbers, whose largest magnitude has the bits `most16`; the scale's e4m3 number in `s8`.
+template <class T>
+__device__ __forceinline__ uint2 codes_of(const uint32_t* w, uint32_t most16, float unscale, uint32_t* s8) {
+  const float most = Two<T>::widen(most16).x * unscale;
   // max|x| has at most 11 significant bits and a tie of e4m3 times 6 has 7, so the quotient, rounded to fp32, is a tie only if it is one.
-  const __nv_fp8_storage_t s8 = __nv_cvt_float_to_fp8(fminf(__fdiv_rn(most, 6.f), 448.f), __NV_SATFINITE, __NV_E4M3);
-  const float s = __half2float(__half(__nv_cvt_fp8_to_halfraw(s8, __NV_E4M3)));
+  *s8 = __nv_cvt_float_to_fp8(fminf(__fdiv_rn(most, 6.f), 448.f), __NV_SATFINITE, __NV_E4M3);
+  const float s = __low2float(cache::scales2(*s8));
   // x 2^-exp / s by the reciprocal is off by 2^-23 at most, which would break ties (0.75 s and the like).  A quotient that is no
   // tie is 2^-11 or more away from one (x has 11 bits at most, s times a tie 7), so rounding to 12 bits (Veltkamp's
   // splitting) puts ties back in place and moves nothing across one.
   const float inv = s > 0.f ? unscale / s : 0.f;
-  const bool over = most > 6.5f * 448.f;         // only then a quotient may pass 7, and much further
   const float2 inv2 = make_float2(inv, inv), split2 = make_float2(4097.f, 4097.f), zero2 = make_float2(0.f, 0.f),
                minus2 = make_float2(-1.f, -1.f);
-  unsigned long long codes = 0;
+  float2 y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = __ffma2_rn(Two<T>::widen(w[i]), inv2, zero2);
+  if (most > 6.5f * 448.f) {                     // only then a quotient may pass 7, and much further
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = make_float2(fminf(fmaxf(y[i].x, -8.f), 8.f), fminf(fmaxf(y[i].y, -8.f), 8.f));
+  }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    float2 y = __ffma2_rn(Two<T>::widen(w[i]), inv2, zero2);
-    if (over) {
-      y.x = fminf(fmaxf(y.x, -8.f), 8.f);
-      y.y = fminf(fmaxf(y.y, -8.f), 8.f);
-    }
-    const float2 c = __ffma2_rn(y, split2, zero2), t = __ffma2_rn(__ffma2_rn(y, minus2, c), minus2, c);
-    codes |= (unsigned long long)__nv_cvt_float2_to_fp4x2(t, __NV_E2M1, cudaRoundNearest) << (8 * i);
+    const float2 c = __ffma2_rn(y[i], split2, zero2);
+    y[i] = __ffma2_rn(__ffma2_rn(y[i], minus2, c), minus2, c);
   }
-  unsigned char* unit = p.data + cache::unit_at<D>(slot, at.head, p.page_shift, p.Hk);
-  const int i = slot % cache::kUnit;
-  if (at.is_value) {
-    unsigned char* dst = unit + U::value_codes(i, at.group);
-    if constexpr (D == 128) {
-      *reinterpret_cast<unsigned long long*>(dst) = codes;
-    } else {
-      *reinterpret_cast<uint32_t*>(dst) = (uint32_t)codes;
-      *reinterpret_cast<uint32_t*>(dst + U::kPartStride) = (uint32_t)(codes >> 32);
+  return make_uint2(pack_codes(*reinterpret_cast<float2(*)[4]>(y)), pack_codes(*reinterpret_cast<float2(*)[4]>(y + 4)));
+}
+
+template <class T, int D>
+__global__ void __launch_bounds__(kThreads) cache_append_kernel(const __grid_constant__ WriteParams p) {
+  using U = cache::Unit<D>;
+  constexpr int kParts = Place<D>::kParts;
+  const Place<D> at(p);
+  kernel_wait();
+  const int slot = at.row < p.rows ? p.slots[at.token] : -1;
+  const bool stored = slot >= 0 && slot < p.slot_end;
+  uint32_t w[2][8], most16[2] = {0, 0};          // largest |x| of each group: 16-bit floats are in the order of their bits
+  if (stored) {
+    const T* src = at.is_value ? (const T*)p.v + at.token * p.v_s[0] + at.head * p.v_s[1]
+                               : (const T*)p.k + at.token * p.k_s[0] + at.head * p.k_s[1];
+    const uint4* in = reinterpret_cast<const uint4*>(src + at.part * 32);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(&w[i / 2][i % 2 * 4]) = in[i];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      uint32_t most2 = w[g][0] & 0x7fff7fffu;
+#pragma unroll
+      for (int i = 1; i < 8; ++i) most2 = __vmaxu2(most2, w[g][i] & 0x7fff7fffu);
+      most16[g] = max(most2 & 0xffffu, most2 >> 16);
     }
-    unit[U::value_scale(i, at.group)] = s8;
+  }
+  // one element that is not finite marks its token's key
+  const bool bad = max(most16[0], most16[1]) >= Two<T>::kInf;
+  const unsigned mine = ((1u << (2 * kParts)) - 1u) << ((threadIdx.x % 32) / (2 * kParts) * (2 * kParts));
+  const bool mark = (__ballot_sync(0xffffffffu, bad) & mine) != 0;
+  if (!stored) return;
+  if (bad) {                                     // such elements count as zero
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      most16[g] = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if ((w[g][i] & 0x7fffu) >= Two<T>::kInf) w[g][i] &= 0xffff0000u;
+        if ((w[g][i] >> 16 & 0x7fffu) >= Two<T>::kInf) w[g][i] &= 0xffffu;
+        most16[g] = max(most16[g], max(w[g][i] & 0x7fffu, w[g][i] >> 16 & 0x7fffu));
+      }
+    }
+  }
+  const float unscale = cache::power2(-(at.is_value ? p.v_exp : p.k_exp));
+  uint32_t s8[2];
+  const uint2 a = codes_of<T>(w[0], most16[0], unscale, s8), b = codes_of<T>(w[1], most16[1], unscale, s8 + 1);
+  unsigned char* unit = p.data + cache::unit_at<D>(slot, at.head, p.page_shift, p.Hk);
+  const int i = slot % cache::kUnit, group = 2 * at.part;
+  if (at.is_value) {
+    unsigned char* dst = unit + U::value_codes(i, group);
+    if constexpr (D == 128) {
+      *reinterpret_cast<uint2*>(dst) = a;
+      *reinterpret_cast<uint2*>(dst + U::kPartStride) = b;       // (a group of 16 channels lies together)
+    } else {
+      *reinterpret_cast<uint32_t*>(dst) = a.x;                   // (8 channels do)
+      *reinterpret_cast<uint32_t*>(dst + U::kPartStride) = a.y;
+      *reinterpret_cast<uint32_t*>(dst + 2 * U::kPartStride) = b.x;
+      *reinterpret_cast<uint32_t*>(dst + 3 * U::kPartStride) = b.y;
+    }
+    unit[U::value_scale(i, group)] = (unsigned char)s8[0];
+    unit[U::value_scale(i, group + 1)] = (unsigned char)s8[1];
   } else {
-    *reinterpret_cast<unsigned long long*>(unit + U::key_codes(i, at.group)) = codes;
-    unit[U::key_scale(i, at.group)] = mark && at.group == 0 ? 0x7f : s8;
+    *reinterpret_cast<uint4*>(unit + U::key_codes(i, group)) = make_uint4(a.x, a.y, b.x, b.y);
+    if (mark && at.part == 0) s8[0] = 0x7f;
+    if constexpr (D == 128) {
+      *reinterpret_cast<unsigned short*>(unit + U::key_scale(i, group)) = (unsigned short)(s8[0] | s8[1] << 8);
+    } else {
+      unit[U::key_scale(i, group)] = (unsigned char)s8[0];
+      unit[U::key_scale(i, group + 1)] = (unsigned char)s8[1];
+    }
   }
 }
 
 template <class T, int D>
-__global__ void __launch_bounds__(kThreads) cache_read_kernel(const WriteParams p) {
+__global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_constant__ WriteParams p) {
   using U = cache::Unit<D>;
-  using cache::Two;
   const Place<D> at(p);
   kernel_wait();
   if (at.row >= p.rows) return;
@@ -120,33 +155,39 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const WriteParams 
   const int slot = p.slots[at.token];
   if (!dst || slot < 0 || slot >= p.slot_end) return;
   const unsigned char* unit = p.data + cache::unit_at<D>(slot, at.head, p.page_shift, p.Hk);
-  const int i = slot % cache::kUnit;
-  unsigned long long codes;
-  uint32_t s8;
+  const int i = slot % cache::kUnit, group = 2 * at.part;
+  uint32_t codes[4], s8[2];
   if (at.is_value) {
-    const unsigned char* src = unit + U::value_codes(i, at.group);
-    if constexpr (D == 128)
-      codes = *reinterpret_cast<const unsigned long long*>(src);
-    else
-      codes = *reinterpret_cast<const uint32_t*>(src) | (unsigned long long)*reinterpret_cast<const uint32_t*>(src + U::kPartStride) << 32;
-    s8 = unit[U::value_scale(i, at.group)];
-  } else {
-    codes = *reinterpret_cast<const unsigned long long*>(unit + U::key_codes(i, at.group));
-    s8 = unit[U::key_scale(i, at.group)];
-  }
-  const float s = __low2float(cache::scales2(s8)) * cache::power2(at.is_value ? p.v_exp : p.k_exp);
-  uint32_t lo[4], hi[4], w[8];
-  cache::codes8((uint32_t)codes, lo);
-  cache::codes8((uint32_t)(codes >> 32), hi);
+    const unsigned char* src = unit + U::value_codes(i, group);
+    if constexpr (D == 128) {
+      *reinterpret_cast<uint2*>(codes) = *reinterpret_cast<const uint2*>(src);
+      *reinterpret_cast<uint2*>(codes + 2) = *reinterpret_cast<const uint2*>(src + U::kPartStride);
+    } else {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float2 f = __half22float2(cache::half2_of(j < 4 ? lo[j % 4] : hi[j % 4]));
-    w[j] = Two<T>::round(f.x * s, f.y * s);
+      for (int x = 0; x < 4; ++x) codes[x] = *reinterpret_cast<const uint32_t*>(src + x * U::kPartStride);
+    }
+    s8[0] = unit[U::value_scale(i, group)];
+    s8[1] = unit[U::value_scale(i, group + 1)];
+  } else {
+    *reinterpret_cast<uint4*>(codes) = *reinterpret_cast<const uint4*>(unit + U::key_codes(i, group));
+    s8[0] = unit[U::key_scale(i, group)];
+    s8[1] = unit[U::key_scale(i, group + 1)];
   }
-  dst += at.is_value ? at.token * p.v_s[0] + at.head * p.v_s[1] : at.token * p.k_s[0] + at.head * p.k_s[1];
-  uint4* out = reinterpret_cast<uint4*>(dst + at.group * 16);
-  out[0] = make_uint4(w[0], w[1], w[2], w[3]);
-  out[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  const float2 both = __half22float2(cache::scales2(s8[0] | s8[1] << 8));
+  const float up = cache::power2(at.is_value ? p.v_exp : p.k_exp);
+  dst += (at.is_value ? at.token * p.v_s[0] + at.head * p.v_s[1] : at.token * p.k_s[0] + at.head * p.k_s[1]) + at.part * 32;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {                  // 8 channels
+    const float s = (x < 2 ? both.x : both.y) * up;
+    uint32_t c[4];
+    cache::codes8(codes[x], c);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 f = __ffma2_rn(__half22float2(cache::half2_of(c[j])), make_float2(s, s), make_float2(0.f, 0.f));
+      c[j] = Two<T>::round(f.x, f.y);
+    }
+    reinterpret_cast<uint4*>(dst)[x] = make_uint4(c[0], c[1], c[2], c[3]);
+  }
 }
 
 enum { kAppend, kRead };
@@ -174,7 +215,7 @@ sol_status_t launch(int what, const sol_attn_cache* c, const void* k, const void
   p.rows = (uint32_t)tokens * (uint32_t)c->Hk;
   p.Hk = c->Hk; p.page_shift = cache::page_shift(c->page_size); p.slot_end = c->pages * c->page_size;
   p.k_exp = c->k_exp; p.v_exp = c->v_exp;
-  const uint32_t per_block = kThreads / (2 * c->d / 16), blocks = (p.rows + per_block - 1) / per_block;
+  const uint32_t per_block = kThreads / (2 * c->d / 32), blocks = (p.rows + per_block - 1) / per_block;
   auto run = [&](auto kernel) {
     return launch_after(kernel, dim3(blocks), kThreads, 0, 0, 0, static_cast<cudaStream_t>(stream), p);
   };

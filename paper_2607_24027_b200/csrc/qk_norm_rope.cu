@@ -23,7 +23,7 @@ struct NormParams {
 };
 
 template <class T, int D>
-__global__ void __launch_bounds__(kWarps * 32) qk_norm_rope_kernel(const NormParams p) {
+__global__ void __launch_bounds__(kWarps * 32, 7) qk_norm_rope_kernel(const __grid_constant__ NormParams p) {
   using cache::Two;
   constexpr int kLanes = D / 8, kRows = 32 / kLanes;
   const int lane = threadIdx.x % 32, sub = lane / kLanes, c0 = (lane % kLanes) * 8;
