@@ -1,9 +1,10 @@
 // Keys and values into the 4-bit cache and back (sol_attn_cache_append, sol_attn_cache_read).
 //
-// Bound by HBM: 4 d bytes of a token and head on one side, 9 d / 8 on the other; and next to that by issuing the instructions, of which
-// finding the place takes as many as 16 channels do.  So a lane has 32 channels of one token, two groups; d / 32 lanes have a key,
-// the next d / 32 the value.
+// Bound by HBM: 4 d bytes of a token and head on one side, 9 d / 8 on the other; next to that by issuing the instructions, of which
+// finding the place takes as many as 16 channels do, and by the L1's accesses.  So a lane has 32 channels of one token, two groups of
+// 32 bytes each, which it loads or stores at once, and a warp's tokens lie side by side.
 #include "cache.cuh"
+#include "ptx_sm100.cuh"
 
 namespace sol {
 namespace {
@@ -17,23 +18,25 @@ struct WriteParams {
   long long k_s[2], v_s[2];
   const int32_t* slots;
   unsigned char* data;
-  uint32_t rows;                                 // tokens * Hk
-  int Hk, page_shift, slot_end, k_exp, v_exp;
+  int tokens, Hk, page_shift, slot_end, k_exp, v_exp;
+  int aligned32;                                 // every row of k and v starts on a 32-byte boundary
 };
 
-// Which row, part of 32 channels and side of a row (key or value) a thread has.
+// Which token, head, part of 32 channels and side (key or value) a thread has.  A warp has 4 (d = 128) or 8 (d = 64) tokens that follow each
+// other in the call, and mostly in the cache too, of one head: then its keys' codes are 256 bytes on end, and its values' fill sectors.
 template <int D>
 struct Place {
-  static constexpr int kParts = D / 32;
-  uint32_t row;
-  int part, token, head;
+  static constexpr int kParts = D / 32, kTokens = 16 / kParts;
+  int part, in_warp, token, head;
   bool is_value;
   __device__ Place(const WriteParams& p) {
-    part = threadIdx.x % kParts;
-    is_value = (threadIdx.x / kParts) % 2;
-    row = blockIdx.x * (kThreads / (2 * kParts)) + threadIdx.x / (2 * kParts);
-    token = (int)(row / (uint32_t)p.Hk);
-    head = (int)(row - (uint32_t)token * p.Hk);
+    const uint32_t lane = threadIdx.x % 32, warp = blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
+    part = lane % kParts;
+    in_warp = lane / kParts % kTokens;
+    is_value = lane >= 16;
+    const uint32_t of = warp / (uint32_t)p.Hk;
+    head = (int)(warp - of * p.Hk);
+    token = (int)(of * kTokens) + in_warp;
   }
 };
 
@@ -81,15 +84,20 @@ __global__ void __launch_bounds__(kThreads) cache_append_kernel(const __grid_con
   constexpr int kParts = Place<D>::kParts;
   const Place<D> at(p);
   kernel_wait();
-  const int slot = at.row < p.rows ? p.slots[at.token] : -1;
+  const int slot = at.token < p.tokens ? p.slots[at.token] : -1;
   const bool stored = slot >= 0 && slot < p.slot_end;
   uint32_t w[2][8], most16[2] = {0, 0};          // largest |x| of each group: 16-bit floats are in the order of their bits
   if (stored) {
     const T* src = at.is_value ? (const T*)p.v + at.token * p.v_s[0] + at.head * p.v_s[1]
                                : (const T*)p.k + at.token * p.k_s[0] + at.head * p.k_s[1];
     const uint4* in = reinterpret_cast<const uint4*>(src + at.part * 32);
+    if (p.aligned32) {
+      ptx::ld_global_v8(in, w[0]);
+      ptx::ld_global_v8(in + 2, w[1]);
+    } else {                                     // the interface only asks for 16 bytes
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(&w[i / 2][i % 2 * 4]) = in[i];
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(&w[i / 2][i % 2 * 4]) = in[i];
+    }
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       uint32_t most2 = w[g][0] & 0x7fff7fffu;
@@ -100,7 +108,7 @@ __global__ void __launch_bounds__(kThreads) cache_append_kernel(const __grid_con
   }
   // one element that is not finite marks its token's key
   const bool bad = max(most16[0], most16[1]) >= Two<T>::kInf;
-  const unsigned mine = ((1u << (2 * kParts)) - 1u) << ((threadIdx.x % 32) / (2 * kParts) * (2 * kParts));
+  const unsigned mine = (((1u << kParts) - 1u) * 0x10001u) << (at.in_warp * kParts);
   const bool mark = (__ballot_sync(0xffffffffu, bad) & mine) != 0;
   if (!stored) return;
   if (bad) {                                     // such elements count as zero
@@ -150,7 +158,7 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_const
   using U = cache::Unit<D>;
   const Place<D> at(p);
   kernel_wait();
-  if (at.row >= p.rows) return;
+  if (at.token >= p.tokens) return;
   T* dst = (T*)const_cast<void*>(at.is_value ? p.v : p.k);
   const int slot = p.slots[at.token];
   if (!dst || slot < 0 || slot >= p.slot_end) return;
@@ -177,16 +185,22 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_const
   const float up = cache::power2(at.is_value ? p.v_exp : p.k_exp);
   dst += (at.is_value ? at.token * p.v_s[0] + at.head * p.v_s[1] : at.token * p.k_s[0] + at.head * p.k_s[1]) + at.part * 32;
 #pragma unroll
-  for (int x = 0; x < 4; ++x) {                  // 8 channels
-    const float s = (x < 2 ? both.x : both.y) * up;
-    uint32_t c[4];
-    cache::codes8(codes[x], c);
+  for (int g = 0; g < 2; ++g) {                  // 16 channels
+    const float s = (g ? both.y : both.x) * up;
+    uint32_t c[8];
+    cache::codes8(codes[2 * g], *reinterpret_cast<uint32_t(*)[4]>(c));
+    cache::codes8(codes[2 * g + 1], *reinterpret_cast<uint32_t(*)[4]>(c + 4));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < 8; ++j) {
       const float2 f = __ffma2_rn(__half22float2(cache::half2_of(c[j])), make_float2(s, s), make_float2(0.f, 0.f));
       c[j] = Two<T>::round(f.x, f.y);
     }
-    reinterpret_cast<uint4*>(dst)[x] = make_uint4(c[0], c[1], c[2], c[3]);
+    if (p.aligned32) {
+      ptx::st_global_v8(dst + g * 16, c);
+    } else {
+      reinterpret_cast<uint4*>(dst + g * 16)[0] = make_uint4(c[0], c[1], c[2], c[3]);
+      reinterpret_cast<uint4*>(dst + g * 16)[1] = make_uint4(c[4], c[5], c[6], c[7]);
+    }
   }
 }
 
@@ -211,11 +225,14 @@ sol_status_t launch(int what, const sol_attn_cache* c, const void* k, const void
   for (int i = 0; i < 2; ++i) { p.k_s[i] = k ? ks[i] : 0; p.v_s[i] = v ? vs[i] : 0; }
   p.slots = slots;
   p.data = static_cast<unsigned char*>(c->data);
-  if ((long long)tokens * c->Hk > 0x7fffffffLL) return SOL_ERR_UNSUPPORTED_SHAPE;
-  p.rows = (uint32_t)tokens * (uint32_t)c->Hk;
+  if ((long long)tokens * c->Hk > 0x3fffffffLL) return SOL_ERR_UNSUPPORTED_SHAPE;
+  p.tokens = tokens;
   p.Hk = c->Hk; p.page_shift = cache::page_shift(c->page_size); p.slot_end = c->pages * c->page_size;
   p.k_exp = c->k_exp; p.v_exp = c->v_exp;
-  const uint32_t per_block = kThreads / (2 * c->d / 32), blocks = (p.rows + per_block - 1) / per_block;
+  p.aligned32 = cache::aligned(k, 32) && cache::aligned(v, 32) &&
+                (p.k_s[0] | p.k_s[1] | p.v_s[0] | p.v_s[1]) % 16 == 0;
+  const uint32_t of_warp = 16 / (c->d / 32), warps = (((uint32_t)tokens + of_warp - 1) / of_warp) * (uint32_t)c->Hk;
+  const uint32_t blocks = (warps + kThreads / 32 - 1) / (kThreads / 32);
   auto run = [&](auto kernel) {
     return launch_after(kernel, dim3(blocks), kThreads, 0, 0, 0, static_cast<cudaStream_t>(stream), p);
   };
