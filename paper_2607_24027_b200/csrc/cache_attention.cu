@@ -442,171 +442,222 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
   if (tid == 0) p.records[blockIdx.x] = record;
 }
 
-// Joins the pieces of the items that several blocks had: block c of the first kernel had the last piece, blocks from record.from to c
-// - 1 the others.  The block that had the first piece left it in its second place, the rest in their first.  A row is added up
+// Joins the pieces of the items that several blocks had: of a kernel's blocks, block c had the last piece, blocks from record.from to c - 1
+// the others.  The block that had the first piece left it in its second place, the rest in their first.  A row is added up
 // by as many warps as it takes for each to have kAtOnce pieces, up to 16, four channels (two, d = 64) to a lane.
-// What bounds this kernel is the way to memory and back, so there are two on its longest path: the records, and up to 8 pieces at once.
-constexpr int kJoinWarps = 16, kAtOnce = 8;
-template <class T, int D, int NB>
-__global__ void __launch_bounds__(32 * kJoinWarps) cache_combine_kernel(const __grid_constant__ AttnParams p, int records) {
-  using C = Cfg<D, NB>;
-  constexpr int kCh = D / 32;
-  __shared__ float joined[kJoinWarps][D + 2];
-  __shared__ int counts[kJoinWarps], spans[kJoinWarps];
-  __shared__ Record list[kMostBlocks];
-  __shared__ short last_of[kMostBlocks];
-  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-  kernel_wait();
-  // the records, packed
+// What bounds this kernel is the way to memory and back, so there are two on its longest path, the records and then the pieces, and
+// registers are kept few, for many rows at once.  One launch joins what both attention kernels left.
+struct Left {                                    // by a kernel
+  const Record* records;
+  const float* parts;
+  int blocks, rows;                              // rows of an item
+};
+constexpr int kJoinWarps = 16;
+struct JoinShared {
+  float joined[kJoinWarps][128 + 2];
+  int counts[kJoinWarps], spans[kJoinWarps];
+  Record list[kMostBlocks];
+  short last_of[kMostBlocks];
+};
+
+// The records with an item, packed: {their number, the most pieces of one}.
+__device__ __forceinline__ int2 pack_records(const Left& left, JoinShared& sh) {
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, blocks = left.blocks;
   int n = 0, most_pieces = 0;
-  for (int c0 = 0; c0 < records; c0 += 32 * kJoinWarps) {
+  for (int c0 = 0; c0 < blocks; c0 += 32 * kJoinWarps) {
     const int c = c0 + tid;
     Record rec{-1, 0, 0, 0, 0, 0, 0, 0};
-    if (c < records) rec = p.records[c];
+    if (c < blocks) rec = left.records[c];
     const unsigned some = __ballot_sync(kAll, rec.from >= 0);
     const int span = __reduce_max_sync(kAll, rec.from >= 0 ? c - rec.from + 1 : 0);
-    if (lane == 0) { counts[warp] = __popc(some); spans[warp] = span; }
+    __syncthreads();                             // (the last round's readers)
+    if (lane == 0) { sh.counts[warp] = __popc(some); sh.spans[warp] = span; }
     __syncthreads();
     int at = n;
     for (int x = 0; x < kJoinWarps; ++x) {
       if (x == warp && rec.from >= 0) {
         const int k = at + __popc(some & ((1u << lane) - 1));
-        list[k] = rec;
-        last_of[k] = (short)c;
+        sh.list[k] = rec;
+        sh.last_of[k] = (short)c;
       }
-      at += counts[x];
-      most_pieces = max(most_pieces, spans[x]);
+      at += sh.counts[x];
+      most_pieces = max(most_pieces, sh.spans[x]);
     }
     n = at;
-    __syncthreads();
   }
+  __syncthreads();
+  return make_int2(n, most_pieces);
+}
+
+// R rows and kAtOnce pieces of each are on their way to a warp together.
+template <class T, int D, int R, int kAtOnce>
+__device__ __forceinline__ void join_items(const AttnParams& p, const Left& left, JoinShared& sh, int n, int most_pieces) {
+  constexpr int kCh = D / 32;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, rows = left.rows;
   int share = 1;
-  while (share < kJoinWarps && share * kAtOnce < most_pieces) share *= 2;
-  const int rows_at_once = kJoinWarps / share;
-  const int tasks = n * C::kRows;
+  if constexpr (R == 1)
+    while (share < kJoinWarps && share * kAtOnce < most_pieces) share *= 2;
+  const int rows_at_once = kJoinWarps / share * R;
+  const int tasks = n * rows, part0 = warp % share;
   for (int t0 = blockIdx.x * rows_at_once; t0 < tasks; t0 += gridDim.x * rows_at_once) {
-    const int task = t0 + warp / share, part0 = warp % share;
+    // (a warp's rows follow each other, and so are of one item: their number is even)
+    const int task = t0 + warp / share * R;
     const bool is = task < tasks;
-    const Record rec = list[is ? task / C::kRows : 0];
-    const int last = last_of[is ? task / C::kRows : 0], row = task % C::kRows;
-    const int full = rec.tile * C::kRows + row;
-    const bool on = is && full < rec.queries * p.group;
-    float top = -INFINITY, sum = 0.f, acc[kCh];
+    const int item = is ? task / rows : 0, row = task - item * rows;
+    const Record& rec = sh.list[item];
+    const int last = sh.last_of[item], from = rec.from, full = rec.tile * rows + row;
+    const int here = is ? min(R, rec.queries * p.group - full) : 0;            // rows that there are (or fewer than one)
+    float top[R], sum[R], acc[R][kCh];
 #pragma unroll
-    for (int i = 0; i < kCh; ++i) acc[i] = 0.f;
-    for (int x0 = rec.from + part0; on && x0 <= last; x0 += share * kAtOnce) {
-      float m[kAtOnce], l[kAtOnce], a[kAtOnce][kCh], most = top;
+    for (int z = 0; z < R; ++z) {
+      top[z] = -INFINITY; sum[z] = 0.f;
+#pragma unroll
+      for (int i = 0; i < kCh; ++i) acc[z][i] = 0.f;
+    }
+    for (int x0 = from + part0; here > 0 && x0 <= last; x0 += share * kAtOnce) {
+      float m[R][kAtOnce], l[R][kAtOnce], a[R][kAtOnce][kCh];
 #pragma unroll
       for (int y = 0; y < kAtOnce; ++y) {
-        const int x = x0 + y * share;
-        const float* part = p.parts + (size_t)(2 * x + (x == rec.from ? 1 : 0)) * C::kPartFloats;
-        m[y] = -INFINITY; l[y] = 0.f;
+        const int x = min(x0 + y * share, last);                               // (what is too much is read and not used)
+        const float* part = left.parts + (size_t)(2 * x + (x == from ? 1 : 0)) * (rows * (D + 2));
 #pragma unroll
-        for (int i = 0; i < kCh; ++i) a[y][i] = 0.f;
-        if (x <= last) {
-          m[y] = part[C::kRows * D + row];
-          l[y] = part[C::kRows * (D + 1) + row];
-          if constexpr (kCh == 4) *reinterpret_cast<float4*>(a[y]) = *reinterpret_cast<const float4*>(part + row * D + lane * 4);
-          else *reinterpret_cast<float2*>(a[y]) = *reinterpret_cast<const float2*>(part + row * D + lane * 2);
+        for (int z = 0; z < R; ++z) {
+          m[z][y] = part[rows * D + row + z];
+          l[z][y] = part[rows * (D + 1) + row + z];
+          if constexpr (kCh == 4) *reinterpret_cast<float4*>(a[z][y]) = *reinterpret_cast<const float4*>(part + (row + z) * D + lane * 4);
+          else *reinterpret_cast<float2*>(a[z][y]) = *reinterpret_cast<const float2*>(part + (row + z) * D + lane * 2);
         }
       }
 #pragma unroll
-      for (int y = 0; y < kAtOnce; ++y) most = fmaxf(most, m[y]);
-      const float f0 = top == -INFINITY ? 1.f : ex2(top - most);               // (then acc and sum are 0 or NaN)
+      for (int z = 0; z < R; ++z) {
+        float most = top[z];
 #pragma unroll
-      for (int i = 0; i < kCh; ++i) acc[i] *= f0;
-      sum *= f0;
-      top = most;
+        for (int y = 0; y < kAtOnce; ++y)
+          if (x0 + y * share <= last) most = fmaxf(most, m[z][y]);
+        const float f0 = top[z] == -INFINITY ? 1.f : ex2(top[z] - most);       // (then acc and sum are 0 or NaN)
 #pragma unroll
-      for (int y = 0; y < kAtOnce; ++y) {
-        const float f = m[y] == -INFINITY ? 1.f : ex2(m[y] - top);             // (a piece without a maximum holds 0 or NaN)
+        for (int i = 0; i < kCh; ++i) acc[z][i] *= f0;
+        sum[z] *= f0;
+        top[z] = most;
 #pragma unroll
-        for (int i = 0; i < kCh; ++i) acc[i] += a[y][i] * f;
-        sum += l[y] * f;
+        for (int y = 0; y < kAtOnce; ++y) {
+          if (x0 + y * share > last) continue;
+          const float f = m[z][y] == -INFINITY ? 1.f : ex2(m[z][y] - most);    // (a piece without a maximum holds 0 or NaN)
+#pragma unroll
+          for (int i = 0; i < kCh; ++i) acc[z][i] += a[z][y][i] * f;
+          sum[z] += l[z][y] * f;
+        }
       }
     }
-    if (share > 1) {
-      __syncthreads();                           // (the last round's readers)
+    if constexpr (R == 1) {
+      if (share > 1) {
+        __syncthreads();                         // (the last round's readers)
 #pragma unroll
-      for (int i = 0; i < kCh; ++i) joined[warp][lane * kCh + i] = acc[i];
-      if (lane == 0) { joined[warp][D] = sum; joined[warp][D + 1] = top; }
-      __syncthreads();
-      if (part0 > 0) continue;
-      float most = lane < share ? joined[warp + lane][D + 1] : -INFINITY;
+        for (int i = 0; i < kCh; ++i) sh.joined[warp][lane * kCh + i] = acc[0][i];
+        if (lane == 0) { sh.joined[warp][D] = sum[0]; sh.joined[warp][D + 1] = top[0]; }
+        __syncthreads();
+        if (part0 > 0) continue;
+        float most = lane < share ? sh.joined[warp + lane][D + 1] : -INFINITY;
 #pragma unroll
-      for (int o = 16; o; o /= 2) most = fmaxf(most, __shfl_xor_sync(kAll, most, o));
-      top = most;
-      sum = 0.f;
+        for (int o = 16; o; o /= 2) most = fmaxf(most, __shfl_xor_sync(kAll, most, o));
+        top[0] = most;
+        sum[0] = 0.f;
 #pragma unroll
-      for (int i = 0; i < kCh; ++i) acc[i] = 0.f;
-      for (int y = warp; y < warp + share; ++y) {
-        const float m = joined[y][D + 1], f = m == -INFINITY ? 1.f : ex2(m - top);
-        sum += joined[y][D] * f;
+        for (int i = 0; i < kCh; ++i) acc[0][i] = 0.f;
+        for (int y = warp; y < warp + share; ++y) {
+          const float m = sh.joined[y][D + 1], f = m == -INFINITY ? 1.f : ex2(m - most);
+          sum[0] += sh.joined[y][D] * f;
 #pragma unroll
-        for (int i = 0; i < kCh; ++i) acc[i] += joined[y][lane * kCh + i] * f;
+          for (int i = 0; i < kCh; ++i) acc[0][i] += sh.joined[y][lane * kCh + i] * f;
+        }
       }
     }
-    if (!on) continue;
-    const int qi = full / p.group, hq = rec.head * p.group + full - qi * p.group;
-    T* dst = (T*)p.out + (rec.first + qi) * p.o_s[0] + hq * p.o_s[1] + lane * kCh;
-    uint32_t w[kCh / 2];
 #pragma unroll
-    for (int i = 0; i < kCh / 2; ++i)
-      w[i] = sum == 0.f ? 0u : Two<T>::round(acc[2 * i] / sum * p.v_scale, acc[2 * i + 1] / sum * p.v_scale);
-    if constexpr (kCh == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
-    else *reinterpret_cast<uint32_t*>(dst) = w[0];
-    if (p.lse && lane == 0)
-      p.lse[(size_t)(rec.first + qi) * p.Hq + hq] = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(sum) - kShift) * kLn2;
+    for (int z = 0; z < R; ++z) {
+      if (z >= here) continue;
+      const int qi = (full + z) / p.group, hq = rec.head * p.group + full + z - qi * p.group;
+      const long long token = rec.first + qi;
+      T* dst = (T*)p.out + token * p.o_s[0] + hq * p.o_s[1] + lane * kCh;
+      const float inv = sum[z] == 0.f ? 0.f : p.v_scale / sum[z];
+      uint32_t w[kCh / 2];
+#pragma unroll
+      for (int i = 0; i < kCh / 2; ++i) w[i] = sum[z] == 0.f ? 0u : Two<T>::round(acc[z][2 * i] * inv, acc[z][2 * i + 1] * inv);
+      if constexpr (kCh == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+      else *reinterpret_cast<uint32_t*>(dst) = w[0];
+      if (p.lse && lane == 0)
+        p.lse[token * p.Hq + hq] = sum[z] == 0.f ? -INFINITY : ((top[z] == -INFINITY ? 0.f : top[z]) + log2f(sum[z]) - kShift) * kLn2;
+    }
   }
 }
 
-template <class T, int D, int NB>
-cudaError_t join(const AttnParams& p, int grid, int sms, cudaStream_t stream, int* n) {
-  const cudaError_t e = launch_after(cache_combine_kernel<T, D, NB>, dim3(2 * sms), 32 * kJoinWarps, 0, 0, 0, stream, p, grid);
-  if (e == cudaSuccess) ++*n;
-  return e;
+// Items with few pieces, as many rows have them, are joined two rows at a time.
+template <class T, int D>
+__global__ void __launch_bounds__(32 * kJoinWarps, 2) cache_combine_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Left few,
+                                                                           const __grid_constant__ Left many) {
+  __shared__ JoinShared sh;
+  kernel_wait();
+#pragma unroll 1
+  for (int kernel = 0; kernel < 2; ++kernel) {
+    const Left& left = kernel ? many : few;
+    if (left.blocks == 0) continue;
+    const int2 found = pack_records(left, sh);
+    if (kernel && found.y <= 6) join_items<T, D, 2, 3>(p, left, sh, found.x, found.y);
+    else join_items<T, D, 1, 5>(p, left, sh, found.x, found.y);
+  }
 }
 
+// The workspace: status word, then for each of the two kernels a record per block and two partial results per block.
+struct Layout {
+  size_t few_records, few_parts, many_records, many_parts, total;
+  Layout(long long rows, int d) {
+    size_t at = 1024;
+    auto take = [&](size_t bytes) { const size_t o = at; at = align_up(at + bytes, 1024); return o; };
+    few_records = take(kMostBlocks * sizeof(Record));
+    few_parts = take(2 * kMostBlocks * (rows <= 8 ? 8 : 16) * (size_t)(d + 2) * sizeof(float));
+    many_records = take(rows <= kFewRows ? 0 : kMostChunkBlocks * sizeof(Record));
+    many_parts = take(rows <= kFewRows ? 0 : 2 * kMostChunkBlocks * kChunkRows * (size_t)(d + 2) * sizeof(float));
+    total = at;
+  }
+};
+
 template <class T, int D, int NB>
-cudaError_t run_few(AttnParams p, long long rows_to, int sms, cudaStream_t stream, int* n) {
+cudaError_t run_few(AttnParams p, long long rows_to, int sms, cudaStream_t stream, Left* left, int* n) {
   using C = Cfg<D, NB>;
   p.rows_from = 0;
   p.rows_to = rows_to;
   int grid = (NB == 1 ? kBlocksPerSm : kBlocksPerSm - 1) * sms;
   if (grid > kMostBlocks) grid = kMostBlocks;
-  const cudaError_t e = launch_after(cache_attention_kernel<T, D, NB>, dim3(grid), kThreads, C::kSmem, C::kSmem, 0, stream, p);
-  if (e != cudaSuccess) return e;
+  *left = Left{p.records, p.parts, grid, C::kRows};
   ++*n;
-  return join<T, D, NB>(p, grid, sms, stream, n);
+  return launch_after(cache_attention_kernel<T, D, NB>, dim3(grid), kThreads, C::kSmem, C::kSmem, 0, stream, p);
 }
 
 template <class T, int D>
-cudaError_t run_many(AttnParams p, long long rows_from, int type, int sms, cudaStream_t stream, int* n) {
-  p.rows_from = rows_from;
-  p.rows_to = kAnyRows;
-  int grid = 0;
-  const cudaError_t e = launch_chunk(p, D, type, sms, stream, &grid);
-  if (e != cudaSuccess) return e;
-  ++*n;
-  return join<T, D, kChunkRows / 8>(p, grid, sms, stream, n);
-}
-
-template <class T, int D>
-cudaError_t run(const AttnParams& p, int max_q, int type, int sms, cudaStream_t stream, int* n) {
+cudaError_t run(AttnParams p, char* ws, int max_q, int type, int sms, cudaStream_t stream, int* n) {
   const long long rows = (long long)max_q * p.group;
-  if (rows <= 8) return run_few<T, D, 1>(p, kAnyRows, sms, stream, n);
-  if (rows <= kFewRows) return run_few<T, D, 2>(p, kAnyRows, sms, stream, n);
-  if (p.requests > 1) {                          // there may be some of either kind
-    const cudaError_t e = run_few<T, D, 2>(p, kFewRows, sms, stream, n);
+  const Layout lay(rows, D);
+  p.records = reinterpret_cast<Record*>(ws + lay.few_records);
+  p.parts = reinterpret_cast<float*>(ws + lay.few_parts);
+  Left few{}, many{};
+  cudaError_t e = cudaSuccess;
+  // With several requests and long ones among them there may be some of either kind.
+  const bool split = rows > kFewRows && p.requests > 1;
+  if (rows <= 8) e = run_few<T, D, 1>(p, kAnyRows, sms, stream, &few, n);
+  else if (rows <= kFewRows || split) e = run_few<T, D, 2>(p, split ? kFewRows : kAnyRows, sms, stream, &few, n);
+  if (e != cudaSuccess) return e;
+  if (rows > kFewRows) {
+    AttnParams q = p;
+    q.records = reinterpret_cast<Record*>(ws + lay.many_records);
+    q.parts = reinterpret_cast<float*>(ws + lay.many_parts);
+    q.rows_from = split ? kFewRows + 1 : 0;
+    q.rows_to = kAnyRows;
+    many = Left{q.records, q.parts, 0, kChunkRows};
+    ++*n;
+    e = launch_chunk(q, D, type, sms, stream, &many.blocks);
     if (e != cudaSuccess) return e;
   }
-  return run_many<T, D>(p, p.requests > 1 ? kFewRows + 1 : 0, type, sms, stream, n);
-}
-
-size_t workspace_bytes(long long rows, int d) {
-  const size_t few = kMostBlocks * sizeof(Record) + 2 * kMostBlocks * (rows <= 8 ? 8 : 16) * (d + 2) * sizeof(float);
-  const size_t many = rows <= kFewRows ? 0 : kMostBlocks * sizeof(Record) + 2 * kMostChunkBlocks * kChunkRows * (size_t)(d + 2) * sizeof(float);
-  return align_up(kRecordsAt + (few > many ? few : many), 1024);
+  ++*n;
+  return launch_after(cache_combine_kernel<T, D>, dim3(2 * sms), 32 * kJoinWarps, 0, 0, 0, stream, p, few, many);
 }
 
 sol_status_t check_attention(const sol_attn_cache_args* a) {
@@ -636,7 +687,7 @@ extern "C" {
 size_t sol_attn_cache_workspace_bytes(int max_q, int Hq, int Hk, int d) {
   if (max_q <= 0 || Hq <= 0 || Hk <= 0 || Hq > sol::cache::kMaxHeads || Hq % Hk || (d != 64 && d != 128)) return 0;
   const long long rows = (long long)max_q * (Hq / Hk);
-  return sol::cache::workspace_bytes(rows, d);
+  return sol::cache::Layout(rows, d).total;
 }
 
 sol_status_t sol_attn_cache_attention(const sol_attn_cache_args* a) {
@@ -664,13 +715,12 @@ sol_status_t sol_attn_cache_attention(const sol_attn_cache_args* a) {
   p.wait_limit = fwd::g_wait_limit;
   p.withhold = fwd::g_withhold_tile;
   p.status = reinterpret_cast<int32_t*>(ws);
-  p.records = reinterpret_cast<cache::Record*>(ws + cache::kRecordsAt);
-  p.parts = reinterpret_cast<float*>(ws + cache::kRecordsAt + cache::kMostBlocks * sizeof(cache::Record));
   const cudaStream_t stream = static_cast<cudaStream_t>(a->stream);
   int n = 0;
   auto typed = [&](auto zero) {
     using T = decltype(zero);
-    return a->cache.d == 128 ? cache::run<T, 128>(p, a->max_q, a->type, sms, stream, &n) : cache::run<T, 64>(p, a->max_q, a->type, sms, stream, &n);
+    return a->cache.d == 128 ? cache::run<T, 128>(p, ws, a->max_q, a->type, sms, stream, &n)
+                             : cache::run<T, 64>(p, ws, a->max_q, a->type, sms, stream, &n);
   };
   const cudaError_t e = a->type == SOL_TYPE_BF16 ? typed(__nv_bfloat16{}) : typed(__half{});
   count_launches(n);

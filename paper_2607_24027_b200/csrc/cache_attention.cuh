@@ -12,8 +12,6 @@ namespace cache {
 constexpr float kShift = 11.f, kMost = 15.f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-// The workspace: status word, a record per block, two partial results per block.  One kernel at a time has it: it is laid out for each.
-constexpr size_t kRecordsAt = 1024;
 constexpr int kMostBlocks = 4 * 160, kMostChunkBlocks = 160;   // of the kernel for few queries, of the other
 constexpr int kChunkRows = 256;                  // rows of a block of the other
 
