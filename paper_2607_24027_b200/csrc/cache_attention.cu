@@ -489,108 +489,132 @@ __device__ __forceinline__ int2 pack_records(const Left& left, JoinShared& sh) {
   return make_int2(n, most_pieces);
 }
 
-// R rows and kAtOnce pieces of each are on their way to a warp together.
-template <class T, int D, int R, int kAtOnce>
-__device__ __forceinline__ void join_items(const AttnParams& p, const Left& left, JoinShared& sh, int n, int most_pieces) {
-  constexpr int kCh = D / 32;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, rows = left.rows;
-  int share = 1;
-  if constexpr (R == 1)
-    while (share < kJoinWarps && share * kAtOnce < most_pieces) share *= 2;
-  const int rows_at_once = kJoinWarps / share * R;
-  const int tasks = n * rows, part0 = warp % share;
-  for (int t0 = blockIdx.x * rows_at_once; t0 < tasks; t0 += gridDim.x * rows_at_once) {
-    // (a warp's rows follow each other, and so are of one item: their number is even)
-    const int task = t0 + warp / share * R;
-    const bool is = task < tasks;
-    const int item = is ? task / rows : 0, row = task - item * rows;
-    const Record& rec = sh.list[item];
-    const int last = sh.last_of[item], from = rec.from, full = rec.tile * rows + row;
-    const int here = is ? min(R, rec.queries * p.group - full) : 0;            // rows that there are (or fewer than one)
-    float top[R], sum[R], acc[R][kCh];
+// Where a row of an item belongs, and what becomes of it: acc[kCh] are its channels from `ch`.
+template <class T, int kCh>
+__device__ __forceinline__ void put_row(const AttnParams& p, const Record& rec, int full, int ch, const float (&acc)[kCh], float sum, float top) {
+  const int qi = full / p.group, hq = rec.head * p.group + full - qi * p.group;
+  const long long token = rec.first + qi;
+  T* dst = (T*)p.out + token * p.o_s[0] + hq * p.o_s[1] + ch;
+  const float inv = sum == 0.f ? 0.f : p.v_scale / sum;
+  uint32_t w[kCh / 2];
 #pragma unroll
-    for (int z = 0; z < R; ++z) {
-      top[z] = -INFINITY; sum[z] = 0.f;
+  for (int i = 0; i < kCh / 2; ++i) w[i] = sum == 0.f ? 0u : Two<T>::round(acc[2 * i] * inv, acc[2 * i + 1] * inv);
+  if constexpr (kCh == 8) *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+  else if constexpr (kCh == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+  else *reinterpret_cast<uint32_t*>(dst) = w[0];
+  if (p.lse && ch == 0)
+    p.lse[token * p.Hq + hq] = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(sum) - kShift) * kLn2;
+}
+
+template <int kCh>
+__device__ __forceinline__ void load_channels(float (&a)[kCh], const float* src) {
+  if constexpr (kCh == 8) {
+    *reinterpret_cast<float4*>(a) = reinterpret_cast<const float4*>(src)[0];
+    *reinterpret_cast<float4*>(a + 4) = reinterpret_cast<const float4*>(src)[1];
+  } else if constexpr (kCh == 4) {
+    *reinterpret_cast<float4*>(a) = *reinterpret_cast<const float4*>(src);
+  } else {
+    *reinterpret_cast<float2*>(a) = *reinterpret_cast<const float2*>(src);
+  }
+}
+
+// acc, sum and top of a row's pieces x0, x0 + every, ... up to `last`, kAtOnce of them on their way together.
+template <int D, int kCh, int kAtOnce>
+__device__ __forceinline__ void add_pieces(const Left& left, int from, int last, int x0, int every, int row, int ch, float (&acc)[kCh], float& sum,
+                                           float& top) {
+  const int rows = left.rows;
+  for (; x0 <= last; x0 += every * kAtOnce) {
+    float m[kAtOnce], l[kAtOnce], a[kAtOnce][kCh], most = top;
 #pragma unroll
-      for (int i = 0; i < kCh; ++i) acc[z][i] = 0.f;
-    }
-    for (int x0 = from + part0; here > 0 && x0 <= last; x0 += share * kAtOnce) {
-      float m[R][kAtOnce], l[R][kAtOnce], a[R][kAtOnce][kCh];
-#pragma unroll
-      for (int y = 0; y < kAtOnce; ++y) {
-        const int x = min(x0 + y * share, last);                               // (what is too much is read and not used)
-        const float* part = left.parts + (size_t)(2 * x + (x == from ? 1 : 0)) * (rows * (D + 2));
-#pragma unroll
-        for (int z = 0; z < R; ++z) {
-          m[z][y] = part[rows * D + row + z];
-          l[z][y] = part[rows * (D + 1) + row + z];
-          if constexpr (kCh == 4) *reinterpret_cast<float4*>(a[z][y]) = *reinterpret_cast<const float4*>(part + (row + z) * D + lane * 4);
-          else *reinterpret_cast<float2*>(a[z][y]) = *reinterpret_cast<const float2*>(part + (row + z) * D + lane * 2);
-        }
-      }
-#pragma unroll
-      for (int z = 0; z < R; ++z) {
-        float most = top[z];
-#pragma unroll
-        for (int y = 0; y < kAtOnce; ++y)
-          if (x0 + y * share <= last) most = fmaxf(most, m[z][y]);
-        const float f0 = top[z] == -INFINITY ? 1.f : ex2(top[z] - most);       // (then acc and sum are 0 or NaN)
-#pragma unroll
-        for (int i = 0; i < kCh; ++i) acc[z][i] *= f0;
-        sum[z] *= f0;
-        top[z] = most;
-#pragma unroll
-        for (int y = 0; y < kAtOnce; ++y) {
-          if (x0 + y * share > last) continue;
-          const float f = m[z][y] == -INFINITY ? 1.f : ex2(m[z][y] - most);    // (a piece without a maximum holds 0 or NaN)
-#pragma unroll
-          for (int i = 0; i < kCh; ++i) acc[z][i] += a[z][y][i] * f;
-          sum[z] += l[z][y] * f;
-        }
-      }
-    }
-    if constexpr (R == 1) {
-      if (share > 1) {
-        __syncthreads();                         // (the last round's readers)
-#pragma unroll
-        for (int i = 0; i < kCh; ++i) sh.joined[warp][lane * kCh + i] = acc[0][i];
-        if (lane == 0) { sh.joined[warp][D] = sum[0]; sh.joined[warp][D + 1] = top[0]; }
-        __syncthreads();
-        if (part0 > 0) continue;
-        float most = lane < share ? sh.joined[warp + lane][D + 1] : -INFINITY;
-#pragma unroll
-        for (int o = 16; o; o /= 2) most = fmaxf(most, __shfl_xor_sync(kAll, most, o));
-        top[0] = most;
-        sum[0] = 0.f;
-#pragma unroll
-        for (int i = 0; i < kCh; ++i) acc[0][i] = 0.f;
-        for (int y = warp; y < warp + share; ++y) {
-          const float m = sh.joined[y][D + 1], f = m == -INFINITY ? 1.f : ex2(m - most);
-          sum[0] += sh.joined[y][D] * f;
-#pragma unroll
-          for (int i = 0; i < kCh; ++i) acc[0][i] += sh.joined[y][lane * kCh + i] * f;
-        }
-      }
+    for (int y = 0; y < kAtOnce; ++y) {
+      const int x = min(x0 + y * every, last);   // (what is too much is read and not used)
+      const float* part = left.parts + (size_t)(2 * x + (x == from ? 1 : 0)) * (rows * (D + 2));
+      m[y] = part[rows * D + row];
+      l[y] = part[rows * (D + 1) + row];
+      load_channels(a[y], part + row * D + ch);
     }
 #pragma unroll
-    for (int z = 0; z < R; ++z) {
-      if (z >= here) continue;
-      const int qi = (full + z) / p.group, hq = rec.head * p.group + full + z - qi * p.group;
-      const long long token = rec.first + qi;
-      T* dst = (T*)p.out + token * p.o_s[0] + hq * p.o_s[1] + lane * kCh;
-      const float inv = sum[z] == 0.f ? 0.f : p.v_scale / sum[z];
-      uint32_t w[kCh / 2];
+    for (int y = 0; y < kAtOnce; ++y)
+      if (x0 + y * every <= last) most = fmaxf(most, m[y]);
+    const float f0 = top == -INFINITY ? 1.f : ex2(top - most);                 // (then acc and sum are 0 or NaN)
 #pragma unroll
-      for (int i = 0; i < kCh / 2; ++i) w[i] = sum[z] == 0.f ? 0u : Two<T>::round(acc[z][2 * i] * inv, acc[z][2 * i + 1] * inv);
-      if constexpr (kCh == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
-      else *reinterpret_cast<uint32_t*>(dst) = w[0];
-      if (p.lse && lane == 0)
-        p.lse[token * p.Hq + hq] = sum[z] == 0.f ? -INFINITY : ((top[z] == -INFINITY ? 0.f : top[z]) + log2f(sum[z]) - kShift) * kLn2;
+    for (int i = 0; i < kCh; ++i) acc[i] *= f0;
+    sum *= f0;
+    top = most;
+#pragma unroll
+    for (int y = 0; y < kAtOnce; ++y) {
+      if (x0 + y * every > last) continue;
+      const float f = m[y] == -INFINITY ? 1.f : ex2(m[y] - most);              // (a piece without a maximum holds 0 or NaN)
+#pragma unroll
+      for (int i = 0; i < kCh; ++i) acc[i] += a[y][i] * f;
+      sum += l[y] * f;
     }
   }
 }
 
-// Items with few pieces, as many rows have them, are joined two rows at a time.
+// Rows with many pieces: as many warps to a row as it takes for each to have kAtOnce, up to 16.
+template <class T, int D>
+__device__ __forceinline__ void join_long(const AttnParams& p, const Left& left, JoinShared& sh, int n, int most_pieces) {
+  constexpr int kCh = D / 32, kAtOnce = 5;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, rows = left.rows;
+  int share = 1;
+  while (share < kJoinWarps && share * kAtOnce < most_pieces) share *= 2;
+  const int rows_at_once = kJoinWarps / share, tasks = n * rows, part0 = warp % share;
+  for (int t0 = blockIdx.x * rows_at_once; t0 < tasks; t0 += gridDim.x * rows_at_once) {
+    const int task = t0 + warp / share;
+    const bool is = task < tasks;
+    const int item = is ? task / rows : 0, row = task - item * rows;
+    const Record& rec = sh.list[item];
+    const int last = sh.last_of[item], full = rec.tile * rows + row;
+    const bool on = is && full < rec.queries * p.group;
+    float top = -INFINITY, sum = 0.f, acc[kCh];
+#pragma unroll
+    for (int i = 0; i < kCh; ++i) acc[i] = 0.f;
+    if (on) add_pieces<D, kCh, kAtOnce>(left, rec.from, last, rec.from + part0, share, row, lane * kCh, acc, sum, top);
+    if (share > 1) {
+      __syncthreads();                           // (the last round's readers)
+#pragma unroll
+      for (int i = 0; i < kCh; ++i) sh.joined[warp][lane * kCh + i] = acc[i];
+      if (lane == 0) { sh.joined[warp][D] = sum; sh.joined[warp][D + 1] = top; }
+      __syncthreads();
+      if (part0 > 0) continue;
+      top = lane < share ? sh.joined[warp + lane][D + 1] : -INFINITY;
+#pragma unroll
+      for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(kAll, top, o));
+      sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < kCh; ++i) acc[i] = 0.f;
+      for (int y = warp; y < warp + share; ++y) {
+        const float m = sh.joined[y][D + 1], f = m == -INFINITY ? 1.f : ex2(m - top);
+        sum += sh.joined[y][D] * f;
+#pragma unroll
+        for (int i = 0; i < kCh; ++i) acc[i] += sh.joined[y][lane * kCh + i] * f;
+      }
+    }
+    if (on) put_row<T>(p, rec, full, lane * kCh, acc, sum, top);
+  }
+}
+
+// Many rows with few pieces: 256 / d rows to a warp, eight channels to a lane, since what a row takes beside its channels is what bounds
+// this (one row to a warp: 286 instructions a row, 19 us for 148 items of 256 rows and 64 channels).
+template <class T, int D>
+__device__ __forceinline__ void join_wide(const AttnParams& p, const Left& left, const JoinShared& sh, int n) {
+  constexpr int kLanes = D / 8, kRowsOfWarp = 32 / kLanes;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, rows = left.rows, tasks = n * rows;
+  const int every = gridDim.x * kJoinWarps * kRowsOfWarp;
+  for (int task = (blockIdx.x * kJoinWarps + warp) * kRowsOfWarp + lane / kLanes; task < tasks; task += every) {
+    const int item = task / rows, row = task - item * rows;
+    const Record& rec = sh.list[item];
+    const int full = rec.tile * rows + row, ch = lane % kLanes * 8;
+    if (full >= rec.queries * p.group) continue;
+    float top = -INFINITY, sum = 0.f, acc[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+    add_pieces<D, 8, 3>(left, rec.from, sh.last_of[item], rec.from, 1, row, ch, acc, sum, top);
+    put_row<T>(p, rec, full, ch, acc, sum, top);
+  }
+}
+
 template <class T, int D>
 __global__ void __launch_bounds__(32 * kJoinWarps, 2) cache_combine_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Left few,
                                                                            const __grid_constant__ Left many) {
@@ -601,8 +625,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 2) cache_combine_kernel(const
     const Left& left = kernel ? many : few;
     if (left.blocks == 0) continue;
     const int2 found = pack_records(left, sh);
-    if (kernel && found.y <= 6) join_items<T, D, 2, 3>(p, left, sh, found.x, found.y);
-    else join_items<T, D, 1, 5>(p, left, sh, found.x, found.y);
+    if (kernel && found.y <= 9) join_wide<T, D>(p, left, sh, found.x);
+    else join_long<T, D>(p, left, sh, found.x, found.y);
   }
 }
 
