@@ -27,8 +27,10 @@ constexpr int kStages = 3;
 constexpr unsigned kAll = 0xffffffffu;
 constexpr int kBlocksPerSm = 4;
 constexpr long long kAnyRows = 1LL << 40;
-// Requests of up to so many rows (queries times the query heads of a key / value head) are this kernel's.
-constexpr long long kFewRows = 64;
+// Requests of up to so many rows (queries times the query heads of a key / value head) are this kernel's.  It takes as long as it has
+// tiles of 16 rows, the other as long for 20 as for 128.  us, this kernel / the other: 16 requests of 8192 keys on 8 heads, 20 rows 93 / 144,
+// 40 rows 129 / 145, 60 rows 173 / 149; one of 32 768 keys 38 / 48, 48 / 49, 55 / 50; 32 of 2048, d = 64, 30 / 50, 37 / 51, 47 / 52.
+constexpr long long kFewRows = 48;
 
 template <int D, int NB>
 struct Cfg {

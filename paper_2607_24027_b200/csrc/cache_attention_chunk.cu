@@ -65,6 +65,8 @@ struct Shared {
   int missing;                                   // a page was not there: from now on softmax looks for itself
 };
 
+static_assert(Cfg<128>::kSmem + sizeof(Shared) <= 227 * 1024, "shared memory of a block");
+
 #define WAIT(bar, parity) mbar_wait_inline((bar), (parity), &sm.abort_flag, p.wait_limit)
 #define WAIT_ALL(bar, parity) __all_sync(kAll, WAIT(bar, parity))
 // (out of line, for the roles that have the registers for a call)
