@@ -461,6 +461,70 @@ def test_replay_streams_and_repetition(sb, new):
     assert sb.sol_attn_cache_read_status(ws) == sb.SOL_OK
 
 
+@pytest.mark.parametrize("requests", [[(1000, 1)] * 3, [(600, 5), (600, 1)], [(900, 300), (500, 1)], [(900, 300)]],
+                         ids=["single tokens", "few rows", "mixed", "many rows"])
+def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_clean(sb, requests):
+    """Each kernel leaves out the arrival for a stage (a test hook): its waits run out, it ends, says so, and leaves nothing behind."""
+    kv, new = [r[0] for r in requests], [r[1] for r in requests]
+    table, cu, pages = batch(kv, new, 16, 3)
+    cache = filled(sb, pages, 16, 2, 128, 4)
+    q = torch.randn(cu[-1], 4, 128, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    ws, out = sb.make_cache_workspace(max(new), 4, 2, 128), torch.empty_like(q)
+    for withheld in (0, 1, 3):
+        sb.sol_attn_debug_set_wait(200_000, withheld)
+        try:
+            sb.sol_attn_cache_attention(q, ints(cu), ints(kv), ints(table), cache, out, max(new), ws)
+            torch.cuda.synchronize()
+        finally:
+            sb.sol_attn_debug_set_wait()
+        # (blocks have a single step here: one stage, or the two tiles of its keys and its values)
+        if withheld == 0 or (withheld == 1 and max(new) > 100):
+            assert sb.sol_attn_cache_read_status(ws) == sb.SOL_ERR_DEVICE_TIMEOUT
+        sb.sol_attn_cache_read_status(ws)
+        assert sb.sol_attn_cache_read_status(ws) == sb.SOL_OK                # cleared by being read
+        check_attention(sb, cache, q, cu, kv, table, True, workspace=ws)
+
+
+def test_calls_on_two_streams_and_from_another_one(sb):
+    """Two calls at once, each with a workspace of its own; the stream given, not the current one, is used."""
+    kv, new = [3000, 700], [1, 80]
+    table, cu, pages = batch(kv, new, 64, 3)
+    cache = filled(sb, pages, 64, 2, 128, 4)
+    g = torch.Generator().manual_seed(1)
+    qs = [torch.randn(cu[-1], 8, 128, generator=g).bfloat16().cuda() for _ in range(2)]
+    args = ints(cu), ints(kv), ints(table)
+    want = [check_attention(sb, cache, q, cu, kv, table, True)[0] for q in qs]
+    streams, spaces, outs = [torch.cuda.Stream() for _ in qs], [sb.make_cache_workspace(80, 8, 2, 128) for _ in qs], [torch.empty_like(q) for q in qs]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for q, st, ws, out in zip(qs, streams, spaces, outs):
+            sb.sol_attn_cache_attention(q, *args, cache, out, 80, ws, stream=st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+@pytest.mark.parametrize("rows", [1, 3, 100])
+def test_unaligned_rows_of_32_bytes(sb, rows):
+    """Rows on 16-byte boundaries only, for every operator that has a path for 32."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    d, H = 64, 2
+    flat = torch.randn(rows * (2 * H * d + 8) + 8, generator=g, device="cuda").bfloat16()
+    k = flat[8:].as_strided((rows, H, d), (2 * H * d + 8, d, 1))
+    v = flat[8 + H * d:].as_strided((rows, H, d), (2 * H * d + 8, d, 1))
+    cache, slots = sb.make_cache(8, 16, H, d), torch.arange(rows, dtype=I32, device="cuda")
+    sb.sol_attn_cache_append(k, v, slots, cache)
+    room = torch.zeros_like(flat)
+    ko, vo = (room[n:].as_strided((rows, H, d), (2 * H * d + 8, d, 1)) for n in (8, 8 + H * d))
+    sb.sol_attn_cache_read(cache, slots, ko, vo)
+    for got, x in ((ko, k), (vo, v)):
+        assert torch.equal(got.cpu().double(), ref.held(x.cpu(), 0)[2])
+    table = [list(range(8))]
+    check_attention(sb, cache, ko, [0, rows], [rows], table, True, values=held_values(cache))
+    sb.sol_attn_qk_norm_rope(ko[None], None, ko[None], None, None, None)
+    want, tol = ref.norm_rope(torch.as_tensor(ref.held(k.cpu(), 0)[2])[None], None, None, None, None, 1e-6, False)
+    close(ko.cpu()[None], want, tol, torch.bfloat16)
+
+
 def test_refusals_of_the_binding(sb):
     cache, q = sb.make_cache(4, 16, 2, 64), torch.zeros(2, 4, 64, dtype=torch.bfloat16, device="cuda")
     cu, kv, table, ws = ints([0, 2]), ints([10]), ints([[0]]), sb.make_cache_workspace(2, 4, 2, 64)
