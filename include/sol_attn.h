@@ -300,7 +300,8 @@ sol_status_t sol_attn_route_materialized(const float* qbar, const float* kc, int
  *   sol_attn_cache_attention   q attends to everything cached (this step's tokens among it)
  * They need no bound workspace, allocate nothing, never synchronise, may be captured and replayed, and are launched with
  * programmatic stream serialization like the kernels above.  (The paper has no counterpart: its kernels see whole sequences.)
- * Index arrays are int32 and 4-byte aligned, everything else 16-byte aligned; strides are in elements; the device pointers
+ * Index arrays are int32 and 4-byte aligned, everything else 16-byte aligned; strides are in elements
+ * (that of a dimension of one is not looked at); the device pointers
  * belong to the current device, `stream` too.  Outputs must not overlap inputs or one another unless an entry says so. */
 
 /* 16-bit element types of the entry points below */
@@ -318,8 +319,9 @@ enum { SOL_TYPE_BF16 = 0, SOL_TYPE_FP16 = 1 };
  *   slots         [max_tokens], out: page * page_size + place in it of each new token; -1 where it has no page (none left, a
  *                 table row that is too short, a negative entry).  Entries from cu_q[requests] on are left as they were
  *   positions     [max_tokens] or NULL, out: position of each new token in its request
- *   result        [2], out: pages that are left, tokens that got no slot.  Must not be free_count itself, which every
- *                 block reads: a caller that loops has two and swaps them.
+ *   result        [2], out: pages that are left, tokens that got no slot
+ * No output may be an input (SOL_ERR_INVALID_ARG where it begins at the same address): every block reads the inputs for itself.  A caller that
+ * loops has two of kv_lens / old_lens and of result / free_count, and swaps them.
  *
  * Pages are taken for the first max_blocks blocks of a request only.  More new tokens than max_tokens: those behind it have no
  * slot and are counted in result[1]. */

@@ -392,14 +392,17 @@ _TYPES = {torch.bfloat16: SOL_TYPE_BF16, torch.float16: SOL_TYPE_FP16}
 _I32, _F32, _U8 = torch.int32, torch.float32, torch.uint8
 
 
-def _device(stream) -> int:
-    at = torch.cuda.current_device()
-    if stream is not None and stream.device.index != at:
-        raise ValueError(f"the stream is not one of the current device ({at})")
-    return at
+def _here(stream):
+    """(current device, address of the stream: the given one, or the device's current one)"""
+    dev = torch.cuda.current_device()
+    if stream is None and _raw_stream is not None:
+        return dev, _raw_stream(dev)
+    if stream is not None and stream.device.index != dev:
+        raise ValueError(f"the stream is not one of the current device ({dev})")
+    return dev, _stream(stream)
 
 
-def _flat(dev, dtype, name, t, *shape) -> int:
+def _flat(dev, dtype, name, t, shape) -> int:
     """The address of a contiguous tensor of this type and shape on device `dev`; 0 for None."""
     if t is None:
         return 0
@@ -417,28 +420,34 @@ def _table(dev, t, B):
 
 
 def _heads(dev, name, t, shape, dtype):
-    """(address, strides but the last) of a tensor of this shape whose channels are contiguous; a stride of a dimension of one counts as 0."""
-    if t.dtype is not dtype or dtype not in _TYPES or t.get_device() != dev or t.shape != shape:
-        raise ValueError(f"{name}: expected a bf16 or fp16 tensor of shape {list(shape)} on the current CUDA device, of one type with the others")
+    """(address, strides) of a tensor of this shape whose channels are contiguous."""
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape:
+        raise ValueError(f"{name}: expected a {dtype} tensor of shape {list(shape)} on the current CUDA device")
     st = t.stride()
-    if st[-1] != 1 and shape[-1] > 1:
+    if st[-1] != 1:
         raise ValueError(f"{name}: the channels are not contiguous")
-    if 1 in shape:
-        st = [x if n > 1 else 0 for x, n in zip(st, shape)]
     return t.data_ptr(), st
+
+
+def _type(dtype) -> int:
+    kind = _TYPES.get(dtype)
+    if kind is None:
+        raise ValueError(f"expected bf16 or fp16 tensors, got {dtype}")
+    return kind
 
 
 def sol_attn_block_tables(old_lens, new_lens, free_pages, free_count, block_tables, cu_q, kv_lens, slots, result, page_size,
                           positions=None, stream=None):
     """Pages, slots and positions of this step's tokens: int32 tensors ``old_lens``, ``new_lens``, ``kv_lens`` [requests], ``cu_q``
     [requests + 1], ``block_tables`` [requests, max_blocks], ``slots`` and ``positions`` [max_tokens], ``free_count`` [1], ``result`` [2]."""
-    dev, B, n, free = _device(stream), old_lens.shape[0], slots.shape[0], free_pages.shape[0]
+    (dev, st), B, n, free = _here(stream), old_lens.shape[0], slots.shape[0], free_pages.shape[0]
     table, table_stride, columns = _table(dev, block_tables, B)
-    a = _PACK_TABLES.pack(_flat(dev, _I32, "old_lens", old_lens, B), _flat(dev, _I32, "new_lens", new_lens, B),
-                          _flat(dev, _I32, "free_pages", free_pages, free), _flat(dev, _I32, "free_count", free_count, 1), table,
-                          _flat(dev, _I32, "cu_q", cu_q, B + 1), _flat(dev, _I32, "kv_lens", kv_lens, B), _flat(dev, _I32, "slots", slots, n),
-                          _flat(dev, _I32, "positions", positions, n), _flat(dev, _I32, "result", result, 2), table_stride, B, columns, n, free,
-                          page_size, _stream(stream))
+    per_request, per_token = (B,), (n,)
+    a = _PACK_TABLES.pack(_flat(dev, _I32, "old_lens", old_lens, per_request), _flat(dev, _I32, "new_lens", new_lens, per_request),
+                          _flat(dev, _I32, "free_pages", free_pages, (free,)), _flat(dev, _I32, "free_count", free_count, (1,)), table,
+                          _flat(dev, _I32, "cu_q", cu_q, (B + 1,)), _flat(dev, _I32, "kv_lens", kv_lens, per_request),
+                          _flat(dev, _I32, "slots", slots, per_token), _flat(dev, _I32, "positions", positions, per_token),
+                          _flat(dev, _I32, "result", result, (2,)), table_stride, B, columns, n, free, page_size, st)
     _check(lib().sol_attn_block_tables(a), "sol_attn_block_tables")
 
 
@@ -450,28 +459,29 @@ def sol_attn_qk_norm_rope(q, k, q_out, k_out, cos, sin, positions=None, q_weight
     x = q if q is not None else k
     if x is None or (q is None) != (q_out is None) or (k is None) != (k_out is None) or (cos is None) != (sin is None):
         raise ValueError("expected q, k or both, each with its output, and cos with sin")
-    dev, dtype, shape = _device(stream), x.dtype, tuple(x.shape)
+    (dev, st), dtype, shape = _here(stream), x.dtype, x.shape
+    kind = _type(dtype)
     if len(shape) != 4:
         raise ValueError("expected tensors of four dimensions")
     token, head = (1, 2) if layout == SOL_LAYOUT_BNHD else (2, 1)
     B, N, d = shape[0], shape[token], shape[3]
-    at, strides, heads = [], [], []
-    for name, a, b in (("q", q, q_out), ("k", k, k_out)):
-        if a is None:
-            at.append((0, 0)), strides.append((0,) * 6), heads.append(0)
-            continue
-        h = a.shape[head] if a.dim() == 4 else 0
-        of = (B, N, h, d) if head == 2 else (B, h, N, d)
-        (pa, sa), (pb, sb) = _heads(dev, name, a, of, dtype), _heads(dev, name + "_out", b, of, dtype)
-        at.append((pa, pb)), heads.append(h)
-        strides.append((sa[0], sa[token], sa[head], sb[0], sb[token], sb[head]))
-    rows, half = (0, 0) if cos is None else cos.shape
-    (q_at, qo_at), (k_at, ko_at) = at
-    (qs, ks) = strides
-    a = _PACK_NORM.pack(q_at, k_at, qo_at, ko_at, *qs[:3], *ks[:3], *qs[3:], *ks[3:], _flat(dev, _F32, "q_weight", q_weight, d),
-                        _flat(dev, _F32, "k_weight", k_weight, d), _flat(dev, _F32, "cos", cos, rows, half),
-                        _flat(dev, _F32, "sin", sin, rows, half), _flat(dev, _I32, "positions", positions, B, N), B, N, *heads, d, 2 * half,
-                        bool(interleaved), rows, _TYPES[dtype], eps, _stream(stream))
+    q_at = qo_at = k_at = ko_at = Hq = Hk = 0
+    qs = qos = ks = kos = (0, 0, 0)
+    if q is not None:
+        Hq = q.shape[head]
+        of = (B, N, Hq, d) if head == 2 else (B, Hq, N, d)
+        (q_at, a), (qo_at, b) = _heads(dev, "q", q, of, dtype), _heads(dev, "q_out", q_out, of, dtype)
+        qs, qos = (a[0], a[token], a[head]), (b[0], b[token], b[head])
+    if k is not None:
+        Hk = k.shape[head]
+        of = (B, N, Hk, d) if head == 2 else (B, Hk, N, d)
+        (k_at, a), (ko_at, b) = _heads(dev, "k", k, of, dtype), _heads(dev, "k_out", k_out, of, dtype)
+        ks, kos = (a[0], a[token], a[head]), (b[0], b[token], b[head])
+    table = (0, 0) if cos is None else cos.shape
+    rows, half = table
+    a = _PACK_NORM.pack(q_at, k_at, qo_at, ko_at, *qs, *ks, *qos, *kos, _flat(dev, _F32, "q_weight", q_weight, (d,)),
+                        _flat(dev, _F32, "k_weight", k_weight, (d,)), _flat(dev, _F32, "cos", cos, table), _flat(dev, _F32, "sin", sin, table),
+                        _flat(dev, _I32, "positions", positions, (B, N)), B, N, Hq, Hk, d, 2 * half, bool(interleaved), rows, kind, eps, st)
     _check(lib().sol_attn_qk_norm_rope(a), "sol_attn_qk_norm_rope")
 
 
@@ -510,14 +520,15 @@ def make_cache(pages, page_size, heads, d, k_exp=0, v_exp=0, device="cuda") -> C
 
 
 def _cache_rows(cache, k, v, slots, stream):
-    dev, x, n = _device(stream), k if k is not None else v, slots.shape[0]
+    (dev, st), x, n = _here(stream), k if k is not None else v, slots.shape[0]
     if x is None:
         raise ValueError("expected k, v or both")
     shape, dtype = (n, cache.heads, cache.d), x.dtype
+    kind = _type(dtype)
     k_at, ks = (0, (0, 0)) if k is None else _heads(dev, "k", k, shape, dtype)
     v_at, vs = (0, (0, 0)) if v is None else _heads(dev, "v", v, shape, dtype)
     return (_PACK_CACHE.pack(*cache.c(dev)), k_at, v_at, _PACK_TWO.pack(ks[0], ks[1]), _PACK_TWO.pack(vs[0], vs[1]),
-            _flat(dev, _I32, "slots", slots, n), n, _TYPES[dtype], _stream(stream))
+            _flat(dev, _I32, "slots", slots, (n,)), n, kind, st)
 
 
 def sol_attn_cache_append(k, v, slots, cache: Cache, stream=None):
@@ -550,17 +561,17 @@ def sol_attn_cache_attention(q, cu_q, kv_lens, block_tables, cache: Cache, out, 
                              stream=None):
     """Attention of ``q`` [tokens, heads, d] (request b: rows cu_q[b] to cu_q[b + 1]) over the first kv_lens[b] tokens of each
     request's pages, into ``out`` (as q) and ``lse`` (fp32 [tokens, heads])."""
-    dev, shape, dtype, B = _device(stream), tuple(q.shape), q.dtype, kv_lens.shape[0]
+    (dev, st), shape, dtype, B = _here(stream), q.shape, q.dtype, kv_lens.shape[0]
+    kind = _type(dtype)
     if len(shape) != 3 or shape[2] != cache.d:
         raise ValueError("expected q of three dimensions, and the cache's d")
     (q_at, qs), (o_at, os_) = _heads(dev, "q", q, shape, dtype), _heads(dev, "out", out, shape, dtype)
     table, table_stride, columns = _table(dev, block_tables, B)
     if workspace.dtype is not _U8 or workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError("workspace: expected a contiguous uint8 tensor on the current CUDA device")
-    a = _PACK_ATTENTION.pack(q_at, o_at, _flat(dev, _F32, "lse", lse, *shape[:2]), qs[0], qs[1], os_[0], os_[1], table_stride,
-                             _flat(dev, _I32, "cu_q", cu_q, B + 1), _flat(dev, _I32, "kv_lens", kv_lens, B), table, *cache.c(dev), shape[0], B,
-                             columns, max_q, shape[1], _TYPES[dtype], bool(causal), scale, workspace.data_ptr(), workspace.numel(),
-                             _stream(stream))
+    a = _PACK_ATTENTION.pack(q_at, o_at, _flat(dev, _F32, "lse", lse, shape[:2]), qs[0], qs[1], os_[0], os_[1], table_stride,
+                             _flat(dev, _I32, "cu_q", cu_q, (B + 1,)), _flat(dev, _I32, "kv_lens", kv_lens, (B,)), table, *cache.c(dev), shape[0],
+                             B, columns, max_q, shape[1], kind, bool(causal), scale, workspace.data_ptr(), workspace.numel(), st)
     _check(lib().sol_attn_cache_attention(a), "sol_attn_cache_attention")
 
 

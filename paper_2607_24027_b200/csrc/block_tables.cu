@@ -138,6 +138,11 @@ extern "C" sol_status_t sol_attn_block_tables(const sol_attn_tables_args* a) {
   if (!a) return SOL_ERR_INVALID_ARG;
   if (a->requests < 0 || a->max_tokens < 0 || a->max_blocks <= 0 || a->free_capacity < 0) return SOL_ERR_INVALID_ARG;
   if (!a->cu_q || !a->result || !a->free_count || a->result == a->free_count || a->result + 1 == a->free_count) return SOL_ERR_INVALID_ARG;
+  // every block reads the inputs for itself, whenever it gets to run: no output may be one of them
+  for (const void* out : {(const void*)a->cu_q, (const void*)a->kv_lens, (const void*)a->slots, (const void*)a->positions, (const void*)a->result,
+                          (const void*)a->block_tables})
+    for (const void* in : {(const void*)a->old_lens, (const void*)a->new_lens, (const void*)a->free_pages, (const void*)a->free_count})
+      if (out && out == in) return SOL_ERR_INVALID_ARG;
   if (a->requests > 0 && (!a->old_lens || !a->new_lens || !a->block_tables || !a->kv_lens)) return SOL_ERR_INVALID_ARG;
   if ((a->max_tokens > 0 && !a->slots) || (a->free_capacity > 0 && !a->free_pages)) return SOL_ERR_INVALID_ARG;
   if (a->table_stride < a->max_blocks) return SOL_ERR_INVALID_ARG;

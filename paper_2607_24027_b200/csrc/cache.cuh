@@ -51,10 +51,9 @@ inline int page_shift(int page_size) {           // of a supported size
   return s;
 }
 inline bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
-inline bool strides_ok(const int64_t* s, int n) {
-  for (int i = 0; i < n; ++i)
-    if (s[i] % 8) return false;
-  return true;
+// Strides of dimensions with more than one entry are multiples of 8 elements.
+inline bool strides_ok(const int64_t* s, int a, int b, int c = 1) {
+  return (a <= 1 || s[0] % 8 == 0) && (b <= 1 || s[1] % 8 == 0) && (c <= 1 || s[2] % 8 == 0);
 }
 
 #ifdef __CUDACC__

@@ -696,7 +696,7 @@ sol_status_t check_attention(const sol_attn_cache_args* a) {
   if (a->Hq > kMaxHeads || a->Hq % a->cache.Hk) return SOL_ERR_UNSUPPORTED_SHAPE;
   if ((long long)a->tokens * (a->Hq / a->cache.Hk) > 0x7fffffffLL) return SOL_ERR_UNSUPPORTED_SHAPE;
   if (a->tokens > 0 && (!a->q || !a->out || !aligned(a->q, 16) || !aligned(a->out, 16))) return SOL_ERR_INVALID_ARG;
-  if (!strides_ok(a->q_stride, 2) || !strides_ok(a->out_stride, 2) || !aligned(a->lse, 4)) return SOL_ERR_INVALID_ARG;
+  if (!strides_ok(a->q_stride, a->tokens, a->Hq) || !strides_ok(a->out_stride, a->tokens, a->Hq) || !aligned(a->lse, 4)) return SOL_ERR_INVALID_ARG;
   if (a->requests > 0 && (!a->cu_q || !a->kv_lens || !a->block_tables)) return SOL_ERR_INVALID_ARG;
   if (!aligned(a->cu_q, 4) || !aligned(a->kv_lens, 4) || !aligned(a->block_tables, 4)) return SOL_ERR_INVALID_ARG;
   const size_t need = sol_attn_cache_workspace_bytes(a->max_q, a->Hq, a->cache.Hk, a->cache.d);

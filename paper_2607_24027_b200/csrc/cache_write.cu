@@ -216,13 +216,17 @@ sol_status_t launch(int what, const sol_attn_cache* c, const void* k, const void
   for (int i = 0; i < 2; ++i) {
     const void* x = i ? v : k;
     const int64_t* st = i ? vs : ks;
-    if (x && (!st || !cache::aligned(x, 16) || !cache::strides_ok(st, 2))) return SOL_ERR_INVALID_ARG;
+    if (x && (!st || !cache::aligned(x, 16) || !cache::strides_ok(st, tokens, c->Hk))) return SOL_ERR_INVALID_ARG;
   }
   if (!slots || !cache::aligned(slots, 4)) return SOL_ERR_INVALID_ARG;
   if ((s = check_device_arch()) != SOL_OK) return s;
   WriteParams p{};
   p.k = k; p.v = v;
-  for (int i = 0; i < 2; ++i) { p.k_s[i] = k ? ks[i] : 0; p.v_s[i] = v ? vs[i] : 0; }
+  for (int i = 0; i < 2; ++i) {                  // (a dimension of one has no use for its stride)
+    const bool one = (i ? c->Hk : tokens) <= 1;
+    p.k_s[i] = k && !one ? ks[i] : 0;
+    p.v_s[i] = v && !one ? vs[i] : 0;
+  }
   p.slots = slots;
   p.data = static_cast<unsigned char*>(c->data);
   if ((long long)tokens * c->Hk > 0x3fffffffLL) return SOL_ERR_UNSUPPORTED_SHAPE;

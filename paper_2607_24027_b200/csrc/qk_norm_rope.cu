@@ -132,8 +132,9 @@ extern "C" sol_status_t sol_attn_qk_norm_rope(const sol_attn_norm_args* a) {
                         (const void*)a->cos, (const void*)a->sin})
     if (!aligned(p, 16)) return SOL_ERR_INVALID_ARG;
   if (!aligned(a->positions, 4)) return SOL_ERR_INVALID_ARG;
-  if ((a->Hq > 0 && !(sol::cache::strides_ok(a->q_stride, 3) && sol::cache::strides_ok(a->q_out_stride, 3))) ||
-      (a->Hk > 0 && !(sol::cache::strides_ok(a->k_stride, 3) && sol::cache::strides_ok(a->k_out_stride, 3))))
+  const int B = a->batch, N = a->tokens;
+  if (!sol::cache::strides_ok(a->q_stride, a->Hq ? B : 0, a->Hq ? N : 0, a->Hq) || !sol::cache::strides_ok(a->q_out_stride, a->Hq ? B : 0, a->Hq ? N : 0, a->Hq) ||
+      !sol::cache::strides_ok(a->k_stride, a->Hk ? B : 0, a->Hk ? N : 0, a->Hk) || !sol::cache::strides_ok(a->k_out_stride, a->Hk ? B : 0, a->Hk ? N : 0, a->Hk))
     return SOL_ERR_INVALID_ARG;
   const sol_status_t s = sol::check_device_arch();
   if (s != SOL_OK) return s;

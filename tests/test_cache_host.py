@@ -124,8 +124,8 @@ def test_bad_norms_are_refused(sb, change, why):
 
 
 def tables_args(sb, **kw):
-    a = dict(old_lens=4096, new_lens=4096, free_pages=4096, free_count=4096, block_tables=4096, cu_q=4096, kv_lens=4096, slots=4096,
-             positions=None, result=8192, table_stride=8, requests=2, max_blocks=8, max_tokens=9, free_capacity=3, page_size=16)
+    a = dict(old_lens=4096, new_lens=4096, free_pages=4096, free_count=4096, block_tables=4 * 4096, cu_q=5 * 4096, kv_lens=6 * 4096,
+             slots=7 * 4096, positions=None, result=8192, table_stride=8, requests=2, max_blocks=8, max_tokens=9, free_capacity=3, page_size=16)
     a.update(kw)
     return sb._TablesArgs(**a)
 
@@ -133,7 +133,8 @@ def tables_args(sb, **kw):
 BAD_TABLES = [(dict(requests=-1), "INVALID"), (dict(max_tokens=-1), "INVALID"), (dict(max_blocks=0), "INVALID"), (dict(free_capacity=-1), "INVALID"),
               (dict(cu_q=None), "INVALID"), (dict(result=None), "INVALID"), (dict(result=4096), "INVALID"), (dict(result=4092), "INVALID"),
               (dict(old_lens=None), "INVALID"), (dict(slots=None), "INVALID"), (dict(free_pages=None), "INVALID"), (dict(table_stride=7), "INVALID"),
-              (dict(page_size=24), "SHAPE"), (dict(page_size=8), "SHAPE"), (dict(kv_lens=4097), "INVALID")]
+              (dict(page_size=24), "SHAPE"), (dict(page_size=8), "SHAPE"), (dict(kv_lens=4097), "INVALID"), (dict(kv_lens=4096), "INVALID"),
+              (dict(old_lens=8192), "INVALID"), (dict(slots=4096), "INVALID"), (dict(block_tables=4096), "INVALID")]
 
 
 @pytest.mark.parametrize("change, why", BAD_TABLES)
@@ -180,10 +181,12 @@ def test_binding_refuses_what_the_kernels_could_not_know(sb):
     with pytest.raises(sb.SolAttnError):
         sb.Cache(torch.zeros(10, dtype=torch.uint8), 4, 24, 2, 128)
     with pytest.raises(ValueError):
-        sb._flat(0, torch.int32, "x", torch.zeros(3, dtype=torch.int32), 3)     # not on a GPU
+        sb._flat(0, torch.int32, "x", torch.zeros(3, dtype=torch.int32), (3,))     # not on a GPU
     with pytest.raises(ValueError):
-        sb._heads(-1, "x", torch.zeros(3, 2, 64), (3, 2, 64), torch.float32)    # not a 16-bit type
-    assert sb._flat(0, torch.int32, "x", None, 3) == 0
+        sb._type(torch.float32)                                                 # not a 16-bit type
+    with pytest.raises(ValueError):
+        sb._heads(-1, "x", torch.zeros(3, 2, 64).half().transpose(1, 2), (3, 64, 2), torch.float16)
+    assert sb._flat(0, torch.int32, "x", None, (3,)) == 0
 
 
 @pytest.mark.parametrize("value, code", [(0.25, 0), (0.26, 1), (0.75, 2), (0.74, 1), (1.25, 2), (1.75, 4), (2.5, 4), (3.5, 6), (5.0, 6), (5.1, 7)])

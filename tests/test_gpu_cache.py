@@ -307,10 +307,12 @@ def test_attention(sb, dtype, page, H, Hk, d, causal, requests):
     check_attention(sb, cache, q, cu, kv, table, causal, scale=0.5 * d ** -0.5)
 
 
-def test_many_requests_and_few(sb):
+@pytest.mark.parametrize("requests, most", [(333, 2), (700, 60)])
+def test_many_requests(sb, requests, most):
+    """More than there are threads to look at their lengths at once, for either kernel."""
     rng = random.Random(2)
-    kv = [rng.choice([1, 5, 16, 100, 300]) for _ in range(333)]
-    new = [rng.choice([1, 1, 1, 0, 2]) for _ in kv]
+    kv = [rng.choice([1, 5, 16, 100, 300]) for _ in range(requests)]
+    new = [rng.choice([1, 1, 1, 0, 2]) if rng.random() < 0.9 else rng.randint(1, most) for _ in kv]
     table, cu, pages = batch(kv, new, 16, 1)
     cache = filled(sb, pages, 16, 2, 64, 4)
     q = torch.randn(cu[-1], 2, 64, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
