@@ -384,7 +384,8 @@ size_t sol_attn_cache_bytes(int pages, int page_size, int Hk, int d);
  * the key's first 16 channels, and every query that sees the token gets NaN (others are not touched).
  *   k, v    [tokens][Hk][d], element strides {token, head}, multiples of 8
  *   slots   int32 [tokens]; a slot outside [0, pages * page_size) is skipped (padding).  Slots that occur must differ: two tokens
- *           for one slot leave a mixture of both there */
+ *           for one slot leave a mixture of both there
+ * tokens * Hk < 2^30. */
 sol_status_t sol_attn_cache_append(const sol_attn_cache* cache /* host */, const void* k, const void* v, const int64_t k_stride[2],
                                    const int64_t v_stride[2], const int32_t* slots, int tokens, int type, sol_stream_t stream);
 
@@ -435,6 +436,8 @@ int64_t sol_attn_launch_count(void);
  * whose "value GEMM finished" signal is left out (withhold_tile < 0: none).  With a tile withheld the
  * waits on that signal run out, every warp role drains, TMEM is released, the kernel returns and
  * sol_attn_read_device_status() reports SOL_ERR_DEVICE_TIMEOUT; the outputs of that launch are invalid.
+ * In the attention kernels over the 4-bit cache the index is that of a block's step whose "bytes are there" signal, or key or value tile
+ * whose "widened" signal, is left out; sol_attn_cache_read_status() reports it.
  * In the routing-bits kernel the index is that of 64 channels whose "products finished" signal is left out; its
  * bits stay right (see sol_attn_route_mask).
  * Nothing faults, traps or spins without a bound.  Not for production use; not thread-safe. */

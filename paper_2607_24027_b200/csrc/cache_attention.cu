@@ -9,6 +9,9 @@
 // A block is four warps; each takes 32 of the 128 keys of a step with softmax statistics of its own, and the four are joined
 // when a piece ends.  The bytes of a step come by one bulk copy (one for each page, if pages are smaller) into a ring,
 // kStages - 1 steps ahead; the warps issue them in turn, which costs each a quarter of the instructions.  Every wait is bounded.
+//
+// One token of 40 heads over 262 143 keys of 8: 67 us, 6.1 TB/s in steady state and 12 us of start and joining; 275 instructions a unit, issue
+// slots 60 % busy, ALU 52 %.  With a copy a lane instead of bulk copies 83 us, with one a warp 78.
 #include <cmath>
 #include <type_traits>
 

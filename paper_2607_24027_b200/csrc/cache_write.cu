@@ -3,6 +3,7 @@
 // Bound by HBM: 4 d bytes of a token and head on one side, 9 d / 8 on the other; next to that by issuing the instructions, of which
 // finding the place takes as many as 16 channels do, and by the L1's accesses.  So a lane has 32 channels of one token, two groups of
 // 32 bytes each, which it loads or stores at once, and a warp's tokens lie side by side.
+// 7800 tokens x 40 heads x 128 channels, slots half taken: writing 46 us (a group to a lane 62, 16-byte loads 54, tokens apart 53), reading 35.
 #include "cache.cuh"
 #include "ptx_sm100.cuh"
 

@@ -4,6 +4,8 @@
 // head and a warp 2 (d = 128) or 4 (d = 64) heads at a time; the partner channels of a pair are in the same lane, or rot / 16
 // lanes further.  A warp keeps to one token, whose cos and sin it reads once for all of its heads.  (Next to HBM comes issuing the
 // instructions: pairs of fp32 numbers go by one, and partners change places as 16-bit pairs.)
+// 72 registers, for 28 warps an SM with four rows each on their way: 32 760 tokens x 80 heads of 128 channels 228 us, 5.9 TB/s; with 88
+// registers 255.
 #include "cache.cuh"
 
 namespace sol {
