@@ -205,13 +205,15 @@ def test_reference_tables():
 
 
 def test_work_shares_cover_everything():
-    """The arithmetic by which the attention kernel deals out its steps and finds who had the others of an item."""
+    """The arithmetic by which the attention kernels deal out their steps and find who had the first piece of an item."""
     rng = random.Random(4)
     for _ in range(2000):
-        work, blocks = rng.randint(1, 10 ** rng.randint(1, 9)), rng.randint(1, 640)
-        blocks = min(blocks, work)
+        work, grid = rng.randint(1, 10 ** rng.randint(1, 11)), rng.randint(1, 640)
+        blocks = min(grid, work)
+        each, extra = work // blocks, work % blocks
+        begin = lambda c: c * each + min(c, extra)  # noqa: E731
         c = rng.randrange(blocks)
-        lo, hi = c * work // blocks, (c + 1) * work // blocks
-        assert hi > lo and (c < blocks - 1 or hi == work)
+        lo, hi = begin(c), begin(c + 1)
+        assert hi - lo in (each, each + 1) and hi > lo and begin(0) == 0 and begin(blocks) == work
         for w in {lo, hi - 1, rng.randrange(lo, hi)}:
-            assert ((w + 1) * blocks - 1) // work == c
+            assert (w // (each + 1) if w < extra * (each + 1) else extra + (w - extra * (each + 1)) // each) == c

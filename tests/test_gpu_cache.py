@@ -319,6 +319,16 @@ def test_many_requests(sb, requests, most):
     check_attention(sb, cache, q, cu, kv, table, True)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("keys, queries, H", [(20000, 64, 1), (20000, 1, 3), (9000, 1, 96), (1300, 7, 40)])
+def test_one_item_among_all_blocks(sb, d, keys, queries, H):
+    """A single key / value head: every block has a piece of the same item, or of one of two; a token with more heads than a tile of rows."""
+    table, cu, pages = batch([keys], [queries], 64, 1)
+    cache = filled(sb, pages, 64, 1, d, 4)
+    q = torch.randn(queries, H, d, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    check_attention(sb, cache, q, cu, [keys], table, True)
+
+
 def test_strides_and_a_larger_hint(sb):
     kv, new = [70, 33], [2, 1]
     table, cu, pages = batch(kv, new, 16, 1)
