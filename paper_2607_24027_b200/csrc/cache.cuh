@@ -90,9 +90,8 @@ __device__ __forceinline__ uint32_t bits(__half2 x) { return *reinterpret_cast<u
 __device__ __forceinline__ __half2 half2_of(uint32_t x) { return *reinterpret_cast<__half2*>(&x); }
 
 // The eight e2m1 numbers of a word, two of a byte to a register (the lower four bits first): exact in fp16.  Written with the word's
-// bytes as operands the conversions need nothing beside them; with words that are
-// shifted first each took one or two more instructions of the same pipe (a loop of them with its multiplications: 26 against 16
-// clocks a word and warp).
+// bytes as operands the conversions need nothing beside them; with words that are shifted first each took one or two more instructions
+// of the same pipe (a loop of them with its multiplications: 26 against 16 clocks a word and warp).
 __device__ __forceinline__ void codes8(uint32_t w, uint32_t (&r)[4]) {
   asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
       "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\tcvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"

@@ -3,8 +3,8 @@
 // Per key and head 9 d / 8 bytes are read for 4 d flops a row, so with few rows HBM is the bound, and next the work of
 // widening: at 6.5 TB/s an SM gets 44 numbers a clock.  A warp widens what it read in registers and multiplies with
 // m16n8k16 products whose 16-sided operand is the cache: S^T = K Q^T (16 keys x 8 rows), O^T = V^T P^T (16 channels x 8 rows),
-// so that a group of up to 8 query heads costs one product, and the cache's layout gives every lane what its
-// operands hold: no exchange, no shared memory for K or V beyond the lane's own staging.
+// so that a group of up to 8 query heads costs one product, and the cache's layout gives every lane what its operands hold: 16 bytes
+// on end of what was copied, no exchange between lanes.
 //
 // A block is four warps; each takes 32 of the 128 keys of a step with softmax statistics of its own, and the four are joined
 // when a piece ends.  The bytes of a step come by one bulk copy (one for each page, if pages are smaller) into a ring,
@@ -90,12 +90,12 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
   using Tiling = Tiles<C::kRows, kStep>;
   const Shares shares = find_share<kThreads, Tiling>(p, blockIdx.x, sh.sums, &sh.start);
   if ((long long)blockIdx.x >= shares.blocks) {
-    if (tid == 0) p.records[blockIdx.x] = Record{-1, 0, 0, 0, 0, 0, 0, 0};
+    if (tid == 0) p.records[blockIdx.x] = kNoRecord;
     return;
   }
   Pieces<Tiling> at;
   at.start(p, sh.start, shares.begin(blockIdx.x), shares.begin(blockIdx.x + 1));
-  Record record{-1, 0, 0, 0, 0, 0, 0, 0};
+  Record record = kNoRecord;
   bool ok = true;
   uint32_t fetches = 0;                          // steps of earlier pieces
 
@@ -380,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
       int never = 0;
       if (!ok)
         for (uint32_t x = n; x < n + kStages; ++x) mbar_wait(&sh.full[x % kStages], (x / kStages) & 1, &never, p.wait_limit);
-      if (tid == 0) p.records[blockIdx.x] = Record{-1, 0, 0, 0, 0, 0, 0, 0};
+      if (tid == 0) p.records[blockIdx.x] = kNoRecord;
       return;
     }
     fetches += (uint32_t)(s_end - s_begin);
@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
       }
     }
     if (!begins && ends)                         // the last piece of a cut item: this block's record has it combined
-      record = Record{(int)shares.owner(at.item_begin), head, tile, r.queries, r.first, 0, 0, 0};
+      record = Record{(int)shares.owner(at.item_begin) | head << 16, tile, r.queries, r.first};
     if (tid == 0) sh.missing = 0;
     fence_proxy_async_smem();                    // the next copies go where the warps' results were
     __syncthreads();
@@ -447,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
   if (tid == 0) p.records[blockIdx.x] = record;
 }
 
-// Joins the pieces of the items that several blocks had: of a kernel's blocks, block c had the last piece, blocks from record.from to c - 1
+// Joins the pieces of the items that several blocks had: of a kernel's blocks, block c had the last piece, blocks from record.from() to c - 1
 // the others.  The block that had the first piece left it in its second place, the rest in their first.  A row is added up
 // by as many warps as it takes for each to have kAtOnce pieces, up to 16, four channels (two, d = 64) to a lane.
 // What bounds this kernel is the way to memory and back, so there are two on its longest path, the records and then the pieces, and
@@ -471,24 +471,27 @@ __device__ __forceinline__ int2 pack_records(const Left& left, JoinShared& sh) {
   int n = 0, most_pieces = 0;
   for (int c0 = 0; c0 < blocks; c0 += 32 * kJoinWarps) {
     const int c = c0 + tid;
-    Record rec{-1, 0, 0, 0, 0, 0, 0, 0};
+    Record rec = kNoRecord;
     if (c < blocks) rec = left.records[c];
-    const unsigned some = __ballot_sync(kAll, rec.from >= 0);
-    const int span = __reduce_max_sync(kAll, rec.from >= 0 ? c - rec.from + 1 : 0);
-    __syncthreads();                             // (the last round's readers)
+    const unsigned some = __ballot_sync(kAll, rec.is());
+    const int span = __reduce_max_sync(kAll, rec.is() ? c - rec.from() + 1 : 0);
+    __syncthreads();                             // (the last pass's readers)
     if (lane == 0) { sh.counts[warp] = __popc(some); sh.spans[warp] = span; }
     __syncthreads();
-    int at = n;
-    for (int x = 0; x < kJoinWarps; ++x) {
-      if (x == warp && rec.from >= 0) {
-        const int k = at + __popc(some & ((1u << lane) - 1));
-        sh.list[k] = rec;
-        sh.last_of[k] = (short)c;
-      }
-      at += sh.counts[x];
-      most_pieces = max(most_pieces, sh.spans[x]);
+    int upto = lane < kJoinWarps ? sh.counts[lane] : 0;          // of warps up to this lane's
+    most_pieces = max(most_pieces, __reduce_max_sync(kAll, lane < kJoinWarps ? sh.spans[lane] : 0));
+#pragma unroll
+    for (int o = 1; o < kJoinWarps; o *= 2) {
+      const int y = __shfl_up_sync(kAll, upto, o);
+      if (lane >= o) upto += y;
     }
-    n = at;
+    const int before = __shfl_sync(kAll, upto, (warp + 31) % 32), total = __shfl_sync(kAll, upto, kJoinWarps - 1);
+    if (rec.is()) {
+      const int k = n + (warp ? before : 0) + __popc(some & ((1u << lane) - 1));
+      sh.list[k] = rec;
+      sh.last_of[k] = (short)c;
+    }
+    n += total;
   }
   __syncthreads();
   return make_int2(n, most_pieces);
@@ -497,7 +500,7 @@ __device__ __forceinline__ int2 pack_records(const Left& left, JoinShared& sh) {
 // Where a row of an item belongs, and what becomes of it: acc[kCh] are its channels from `ch`.
 template <class T, int kCh>
 __device__ __forceinline__ void put_row(const AttnParams& p, const Record& rec, int full, int ch, const float (&acc)[kCh], float sum, float top) {
-  const int qi = full / p.group, hq = rec.head * p.group + full - qi * p.group;
+  const int qi = full / p.group, hq = rec.head() * p.group + full - qi * p.group;
   const long long token = rec.first + qi;
   T* dst = (T*)p.out + token * p.o_s[0] + hq * p.o_s[1] + ch;
   const float inv = sum == 0.f ? 0.f : p.v_scale / sum;
@@ -575,9 +578,9 @@ __device__ __forceinline__ void join_long(const AttnParams& p, const Left& left,
     float top = -INFINITY, sum = 0.f, acc[kCh];
 #pragma unroll
     for (int i = 0; i < kCh; ++i) acc[i] = 0.f;
-    if (on) add_pieces<D, kCh, kAtOnce>(left, rec.from, last, rec.from + part0, share, row, lane * kCh, acc, sum, top);
+    if (on) add_pieces<D, kCh, kAtOnce>(left, rec.from(), last, rec.from() + part0, share, row, lane * kCh, acc, sum, top);
     if (share > 1) {
-      __syncthreads();                           // (the last round's readers)
+      __syncthreads();                           // (the last pass's readers)
 #pragma unroll
       for (int i = 0; i < kCh; ++i) sh.joined[warp][lane * kCh + i] = acc[i];
       if (lane == 0) { sh.joined[warp][D] = sum; sh.joined[warp][D + 1] = top; }
@@ -615,7 +618,7 @@ __device__ __forceinline__ void join_wide(const AttnParams& p, const Left& left,
     float top = -INFINITY, sum = 0.f, acc[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i] = 0.f;
-    add_pieces<D, 8, 3>(left, rec.from, sh.last_of[item], rec.from, 1, row, ch, acc, sum, top);
+    add_pieces<D, 8, 3>(left, rec.from(), sh.last_of[item], rec.from(), 1, row, ch, acc, sum, top);
     put_row<T>(p, rec, full, ch, acc, sum, top);
   }
 }

@@ -17,7 +17,13 @@ constexpr int kChunkRows = 256;                  // rows of a block of the other
 
 // An item of which a block had the last piece and others the rest: the first of them (-1: there is no such item), and where its rows
 // belong.
-struct alignas(32) Record { int from, head, tile, queries, first, pad0, pad1, pad2; };
+struct alignas(16) Record {
+  int from_head, tile, queries, first;           // from | head << 16
+  __host__ __device__ bool is() const { return from_head >= 0; }
+  __host__ __device__ int from() const { return from_head & 0xffff; }
+  __host__ __device__ int head() const { return from_head >> 16; }
+};
+#define kNoRecord (Record{-1, 0, 0, 0})
 
 struct AttnParams {
   const void* q;
@@ -43,7 +49,8 @@ __device__ __forceinline__ Request request_at(const AttnParams& p, int b) {
   Request r;
   r.first = max(0, min(p.cu_q[b], p.tokens));
   r.queries = max(0, min(p.cu_q[b + 1], p.tokens) - r.first);
-  r.keys = (int)max(0LL, min((long long)p.kv_lens[b], (long long)p.max_blocks << p.page_shift));
+  // (0x7fff0000: sums with a step stay within 32 bits; a cache has fewer tokens than 2^31)
+  r.keys = (int)max(0LL, min(min((long long)p.kv_lens[b], (long long)p.max_blocks << p.page_shift), 0x7fff0000LL));
   return r;
 }
 

@@ -1,5 +1,5 @@
-// Attention of many queries over the 4-bit cache (sol_attn_cache_attention): prompts, chunks of a video.  TMA is of no use here,
-// since what the tensor core multiplies is not in memory: warps widen the cache's pages into shared memory.
+// Attention of many queries over the 4-bit cache (sol_attn_cache_attention): prompts, chunks of a video.  What the tensor core multiplies is
+// not in memory, so tiled TMA loads have nothing to bring: bulk copies bring the cache's units, and warps widen them into the tiles.
 //
 // A row is one query of one of the query heads that share a key / value head.  A block has two tiles of 128 rows, so that what is widened
 // once is multiplied by 256 rows, and the two tiles take turns on the tensor core and the special-function units as in
@@ -294,8 +294,8 @@ __device__ void mma_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at, un
   bool first = true;
   while (ok && next_piece(at, p, lane)) {
     if (first && lane == 0) {                    // the last piece of a cut item is a block's first
-      Record record{-1, 0, 0, 0, 0, 0, 0, 0};
-      if (!at.begins() && at.ends()) record = Record{(int)shares.owner(at.item_begin), at.head, at.tile, at.r.queries, at.r.first, 0, 0, 0};
+      Record record = kNoRecord;
+      if (!at.begins() && at.ends()) record = Record{(int)shares.owner(at.item_begin) | at.head << 16, at.tile, at.r.queries, at.r.first};
       p.records[blockIdx.x] = record;
     }
     first = false;
@@ -596,7 +596,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_chunk_kernel(cons
       else widen_role<D>(sm, p, (uint32_t)(shares.begin(blockIdx.x + 1) - shares.begin(blockIdx.x)), sKV, sRaw, warp - kWarpWiden, lane);
     }
   } else if (threadIdx.x == 0) {
-    p.records[blockIdx.x] = Record{-1, 0, 0, 0, 0, 0, 0, 0};
+    p.records[blockIdx.x] = kNoRecord;
   }
   tc_fence_before();
   __syncthreads();
