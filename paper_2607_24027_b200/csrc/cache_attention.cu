@@ -10,7 +10,7 @@
 // when a piece ends.  The bytes of a step come by one bulk copy (one for each page, if pages are smaller) into a ring,
 // kStages - 1 steps ahead; the warps issue them in turn, which costs each a quarter of the instructions.  Every wait is bounded.
 //
-// One token of 40 heads over 262 143 keys of 8: 67 us, 6.1 TB/s in steady state and 12 us of start and joining; 275 instructions a unit, issue
+// One token of 40 heads over 262 143 keys of 8: 65 us, 6.1 TB/s in steady state and 10 us of start and joining; 275 instructions a unit, issue
 // slots 60 % busy, ALU 52 %.  With a copy a lane instead of bulk copies 83 us, with one a warp 78.
 #include <cmath>
 #include <type_traits>
