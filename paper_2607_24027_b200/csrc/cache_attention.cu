@@ -90,12 +90,12 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
   using Tiling = Tiles<C::kRows, kStep>;
   const Shares shares = find_share<kThreads, Tiling>(p, blockIdx.x, sh.sums, &sh.start);
   if ((long long)blockIdx.x >= shares.blocks) {
-    if (tid == 0) p.records[blockIdx.x] = kNoRecord;
+    if (tid == 0) p.records[blockIdx.x] = Record::none();
     return;
   }
   Pieces<Tiling> at;
   at.start(p, sh.start, shares.begin(blockIdx.x), shares.begin(blockIdx.x + 1));
-  Record record = kNoRecord;
+  Record record = Record::none();
   bool ok = true;
   uint32_t fetches = 0;                          // steps of earlier pieces
 
@@ -380,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
       int never = 0;
       if (!ok)
         for (uint32_t x = n; x < n + kStages; ++x) mbar_wait(&sh.full[x % kStages], (x / kStages) & 1, &never, p.wait_limit);
-      if (tid == 0) p.records[blockIdx.x] = kNoRecord;
+      if (tid == 0) p.records[blockIdx.x] = Record::none();
       return;
     }
     fetches += (uint32_t)(s_end - s_begin);
@@ -471,7 +471,7 @@ __device__ __forceinline__ int2 pack_records(const Left& left, JoinShared& sh) {
   int n = 0, most_pieces = 0;
   for (int c0 = 0; c0 < blocks; c0 += 32 * kJoinWarps) {
     const int c = c0 + tid;
-    Record rec = kNoRecord;
+    Record rec = Record::none();
     if (c < blocks) rec = left.records[c];
     const unsigned some = __ballot_sync(kAll, rec.is());
     const int span = __reduce_max_sync(kAll, rec.is() ? c - rec.from() + 1 : 0);

@@ -8,7 +8,7 @@ namespace sol {
 namespace cache {
 
 // Weights are 2^(x - m + kShift) with x the logit times log2(e) and m a maximum of earlier keys, which is replaced once a weight would
-// pass 2^kMost: fp16 holds them to 2^-12 down to 2^-25 of the largest, and is off by 2^-36 of it at most below.
+// pass 2^kMost: fp16 holds them to 2^-11 down to 2^-25 of the largest, and is off by 2^-36 of it at most below.
 constexpr float kShift = 11.f, kMost = 15.f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -22,8 +22,8 @@ struct alignas(16) Record {
   __host__ __device__ bool is() const { return from_head >= 0; }
   __host__ __device__ int from() const { return from_head & 0xffff; }
   __host__ __device__ int head() const { return from_head >> 16; }
+  __host__ __device__ static Record none() { return Record{-1, 0, 0, 0}; }
 };
-#define kNoRecord (Record{-1, 0, 0, 0})
 
 struct AttnParams {
   const void* q;

@@ -294,7 +294,7 @@ __device__ void mma_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at, un
   bool first = true;
   while (ok && next_piece(at, p, lane)) {
     if (first && lane == 0) {                    // the last piece of a cut item is a block's first
-      Record record = kNoRecord;
+      Record record = Record::none();
       if (!at.begins() && at.ends()) record = Record{(int)shares.owner(at.item_begin) | at.head << 16, at.tile, at.r.queries, at.r.first};
       p.records[blockIdx.x] = record;
     }
@@ -596,7 +596,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_chunk_kernel(cons
       else widen_role<D>(sm, p, (uint32_t)(shares.begin(blockIdx.x + 1) - shares.begin(blockIdx.x)), sKV, sRaw, warp - kWarpWiden, lane);
     }
   } else if (threadIdx.x == 0) {
-    p.records[blockIdx.x] = kNoRecord;
+    p.records[blockIdx.x] = Record::none();
   }
   tc_fence_before();
   __syncthreads();
