@@ -398,7 +398,8 @@ sol_status_t sol_attn_cache_read(const sol_attn_cache* cache /* host */, void* k
  * first kv_lens[b] tokens of its block table (clamped to max_blocks * page_size).  With `causal`, query i of n sees the first
  * kv_len - n + i + 1 tokens, else all.  Query head h uses key / value head h / (Hq / Hk).
  *
- *   q, out       [tokens][Hq][d], element strides {token, head}, multiples of 8; rows outside the requests are neither read nor written
+ *   q, out       [tokens][Hq][d], element strides {token, head}, multiples of 8; rows outside the requests are neither read nor written; out may not
+ *                be q (SOL_ERR_INVALID_ARG)
  *   lse          fp32 [tokens][Hq] contiguous or NULL, out: natural log of the sum of exp(scale q.k)
  *   block_tables [requests][max_blocks], rows table_stride apart; tokens of a page outside [0, pages) are not seen
  *   max_q        the longest request's number of queries: chooses the kernel; a longer one is still computed

@@ -701,6 +701,7 @@ sol_status_t check_attention(const sol_attn_cache_args* a) {
   if (std::isnan(a->scale) || std::isinf(a->scale) || a->table_stride < a->max_blocks) return SOL_ERR_INVALID_ARG;
   if (a->Hq > kMaxHeads || a->Hq % a->cache.Hk) return SOL_ERR_UNSUPPORTED_SHAPE;
   if ((long long)a->tokens * (a->Hq / a->cache.Hk) > 0x7fffffffLL) return SOL_ERR_UNSUPPORTED_SHAPE;
+  if (a->tokens > 0 && a->q == a->out) return SOL_ERR_INVALID_ARG;             // several blocks read a row's queries
   if (a->tokens > 0 && (!a->q || !a->out || !aligned(a->q, 16) || !aligned(a->out, 16))) return SOL_ERR_INVALID_ARG;
   if (!strides_ok(a->q_stride, a->tokens, a->Hq) || !strides_ok(a->out_stride, a->tokens, a->Hq) || !aligned(a->lse, 4)) return SOL_ERR_INVALID_ARG;
   if (a->requests > 0 && (!a->cu_q || !a->kv_lens || !a->block_tables)) return SOL_ERR_INVALID_ARG;

@@ -79,7 +79,7 @@ def attention_args(sb, cache=None, **kw):
 
 BAD_ATTENTION = [(dict(tokens=-1), "INVALID"), (dict(requests=-1), "INVALID"), (dict(max_q=0), "INVALID"), (dict(max_blocks=0), "INVALID"),
                  (dict(type=3), "INVALID"), (dict(scale=float("nan")), "INVALID"), (dict(scale=float("inf")), "INVALID"),
-                 (dict(table_stride=7), "INVALID"), (dict(q=None), "INVALID"), (dict(out=4104), "INVALID"), (dict(cu_q=None), "INVALID"),
+                 (dict(table_stride=7), "INVALID"), (dict(q=None), "INVALID"), (dict(out=4104), "INVALID"), (dict(out=4096), "INVALID"), (dict(cu_q=None), "INVALID"),
                  (dict(kv_lens=4097), "INVALID"), (dict(block_tables=None), "INVALID"), (dict(lse=4097), "INVALID"), (dict(Hq=0), "INVALID"),
                  (dict(Hq=5), "SHAPE"), (dict(Hq=2048), "SHAPE"), (dict(workspace=None), "WORKSPACE"), (dict(workspace=4096 + 16), "WORKSPACE"),
                  (dict(workspace_bytes=4096), "WORKSPACE"), (dict(q_stride=(ctypes.c_int64 * 2)(512, 4)), "INVALID")]

@@ -152,7 +152,8 @@ def same(a, b):
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("T, H, d, page, k_exp, v_exp", [(1, 1, 64, 16, 0, 0), (5, 3, 128, 16, 2, -3), (33, 8, 128, 64, 0, 1), (130, 2, 64, 32, -4, 0),
-                                                         (517, 5, 64, 256, 0, 0), (257, 1, 128, 128, -1, 7)])
+                                                         (517, 5, 64, 256, 0, 0), (257, 1, 128, 128, -1, 7),
+                                                         (40, 2, 128, 16, 64, -64)])
 def test_append_and_read(sb, dtype, T, H, d, page, k_exp, v_exp):
     g = torch.Generator().manual_seed(T * d)
     pages = -(-T // page) + 2
@@ -603,3 +604,46 @@ def test_a_generator(sb, dtype, H, Hk, d, page):
         assert touched.all()
         close(out, want, tol, dtype)
         lens = kv
+
+
+def test_a_captured_step(sb):
+    """A decoding step of all four operators as one graph, replayed step after step with what a program changes between them."""
+    B, H, Hk, d, page, width, pages = 5, 8, 2, 128, 16, 6, 40
+    g = torch.Generator().manual_seed(3)
+    start = [3, 15, 16, 40, 0]
+    cos, sin = (x.cuda() for x in rotation(width * page, d))
+    free = torch.arange(pages, dtype=I32, device="cuda")
+
+    def fresh():
+        s = dict(old=ints(start), new=ints([1] * B), count=ints([pages - 5 * 3]), table=torch.full((B, width), -1, dtype=I32, device="cuda"),
+                 cache=filled(sb, pages, page, Hk, d, 6), cu=ints([0] * (B + 1)), kv=ints([0] * B), slots=ints([0] * B), pos=ints([0] * B),
+                 result=ints([0, 0]), ws=sb.make_cache_workspace(1, H, Hk, d))
+        s["table"][:, :3] = torch.arange(pages - 15, pages, dtype=I32).view(B, 3).cuda()
+        s.update({n: torch.zeros(B, h, d, dtype=torch.bfloat16, device="cuda") for n, h in (("q", H), ("k", Hk), ("v", Hk), ("qr", H), ("kr", Hk), ("out", H))})
+        return s
+
+    def step(s):
+        sb.sol_attn_block_tables(s["old"], s["new"], free, s["count"], s["table"], s["cu"], s["kv"], s["slots"], s["result"], page, positions=s["pos"])
+        sb.sol_attn_qk_norm_rope(s["q"][None], s["k"][None], s["qr"][None], s["kr"][None], cos, sin, positions=s["pos"][None])
+        sb.sol_attn_cache_append(s["kr"], s["v"], s["slots"], s["cache"])
+        sb.sol_attn_cache_attention(s["qr"], s["cu"], s["kv"], s["table"], s["cache"], s["out"], 1, s["ws"])
+
+    plain, graphed = fresh(), fresh()
+    step(fresh())
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step(graphed)
+    for _ in range(20):
+        x = [torch.randn(B, h, d, generator=g).bfloat16() for h in (H, Hk, Hk)]
+        for s in (plain, graphed):
+            for n, y in zip(("q", "k", "v"), x):
+                s[n].copy_(y)
+        step(plain)
+        graph.replay()
+        for n in ("table", "kv", "slots", "pos", "result", "out"):
+            assert torch.equal(plain[n], graphed[n]), n
+        assert torch.equal(plain["cache"].data, graphed["cache"].data) and not plain["out"].isnan().any()
+        for s in (plain, graphed):                                         # the next step: lengths and the count move on
+            s["old"].copy_(s["kv"]), s["count"].copy_(s["result"][:1])
+    assert plain["kv"].tolist() == [n + 20 for n in start]
