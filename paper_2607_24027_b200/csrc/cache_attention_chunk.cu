@@ -11,7 +11,7 @@
 //   loader   (warp 9) the cache's units of 16 tokens into a ring of 14
 //   widen    (warps 10-15) units to fp16 tiles in a ring of four slots, K0 V0 K1 V1 ..., in the 128-byte swizzle that the tensor core reads
 // The cache's values are exact in fp16, so K and V enter the products unrounded.
-// 37 heads x 1024 queries x 32 768 keys, d = 128: 564 us, 1126 TFLOP/s; a step of 256 rows x 128 keys 2.04 us (d = 64 1.90), which is what
+// 37 heads x 1024 queries x 32 768 keys, d = 128: 564 us, 1126 TFLOP/s; a step of 256 rows x 128 keys 2.04 us (d = 64 1.75), which is what
 // fwd_sm100_dense.cu takes with tiles that TMA brings: one tile's softmax, P V and Q K^T follow one another.  Tensor pipe 49 % busy.
 //
 // TMEM: S_A [0, 128)  S_B [128, 256)  O_A [256, 256 + d)  O_B [256 + d, 256 + 2 d).  Every wait is bounded.
@@ -83,6 +83,32 @@ __device__ __forceinline__ void flag_timeout(Shared& sm, const AttnParams& p) {
 // Instruction descriptor for kind::f16 with fp16 A / B and fp32 accumulation (see make_idesc_bf16).
 __host__ __device__ constexpr uint32_t make_idesc_f16(int M, int N, bool b_mn_major) {
   return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+// Maximum of three; if kNaN, NaN if one is.
+template <bool kNaN>
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  if constexpr (!kNaN) return fmaxf(fmaxf(a, b), c);
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+// 2^x of two numbers up to 2^7 on the FMA pipe: x = n + f with n the nearest integer (x plus 1.5 * 2^23 rounds there), 2^f by the polynomial of
+// degree 4 whose largest relative error on [-1/2, 1/2] is least (2.6e-6, by a linear program), n added to the exponent.
+// Below -126 it is 2^-126.  Not for NaN.
+__device__ __forceinline__ float2 exp2_fma(float2 x) {
+  x = make_float2(fmaxf(x.x, -126.f), fmaxf(x.y, -126.f));
+  const float2 magic = make_float2(12582912.f, 12582912.f), minus = make_float2(-12582912.f, -12582912.f);
+  const float2 t = __fadd2_rn(x, magic), n = __fadd2_rn(t, minus);
+  const float2 f = __ffma2_rn(n, make_float2(-1.f, -1.f), x);
+  float2 q = make_float2(0.00956970546f, 0.00956970546f);
+  q = __ffma2_rn(q, f, make_float2(0.0559181989f, 0.0559181989f));
+  q = __ffma2_rn(q, f, make_float2(0.240247652f, 0.240247652f));
+  q = __ffma2_rn(q, f, make_float2(0.693121731f, 0.693121731f));
+  q = __ffma2_rn(q, f, make_float2(0.999999225f, 0.999999225f));
+  return make_float2(__uint_as_float(__float_as_uint(q.x) + (__float_as_uint(t.x) << 23)),
+                     __uint_as_float(__float_as_uint(q.y) + (__float_as_uint(t.y) << 23)));
 }
 
 // Row tiles of a piece that have rows.
@@ -352,6 +378,9 @@ __device__ void softmax_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at
                              int warp_in_group, int lane) {
   using C = Cfg<D>;
   constexpr int kHalf = kCols / 2;
+  // With 64 channels the exponentials, not the tensor core, are what a step waits for, and a quarter of them goes to the FMA pipe: 1.75
+  // instead of 1.90 us a step.  With 128 the instructions cost more than they free: 2.27 instead of 2.06.
+  constexpr bool kPoly = D == 64;
   const uint32_t lane_base = tmem + ((uint32_t)(warp_in_group * 32) << 16);
   const uint32_t t_s = lane_base + kTmemS + s * kCols, t_o = lane_base + kTmemO + s * D;
   const int row = warp_in_group * 32 + lane;
@@ -438,8 +467,8 @@ __device__ void softmax_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at
         for (int c = 0; c < kQ; c += 2)
 #pragma unroll
           for (int x = 0; x < 4; ++x)
-            m[x] = fmaxf(fmaxf(m[x], __uint_as_float(sr[c0 + x * kQ + c])), __uint_as_float(sr[c0 + x * kQ + c + 1]));
-        return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+            m[x] = max3<kPoly>(m[x], __uint_as_float(sr[c0 + x * kQ + c]), __uint_as_float(sr[c0 + x * kQ + c + 1]));
+        return max3<kPoly>(max3<kPoly>(m[0], m[1], m[2]), m[3], m[3]);
       };
       // the maximum of the first half is taken while the second half is on its way
       tmem_ld_cols<kHalf>(t_s, sr);
@@ -447,8 +476,8 @@ __device__ void softmax_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at
       tmem_ld_cols<kHalf>(t_s + kHalf, sr + kHalf);
       float mx = half_max(0);
       tmem_ld_wait();
-      mx = fmaxf(mx, half_max(kHalf));
-      mx *= sl2;                                 // (NaN is not among what the maximum is taken of)
+      mx = max3<kPoly>(mx, half_max(kHalf), mx) * sl2;           // (without the polynomial NaN is not among what the maximum is taken of)
+      if (kPoly && mx != mx) l = NAN;            // (a key that the row sees is not finite: the polynomial's weight for it may be any number)
       const bool some = mx > -INFINITY;
       if (__any_sync(kAll, some && (!seen || mx + nm > kMost))) {
         const float nm_new = some && (!seen || mx + nm > kMost) ? kShift - mx : nm;
@@ -479,7 +508,7 @@ __device__ void softmax_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at
           const float2 xa = __ffma2_rn(make_float2(__uint_as_float(x[0]), __uint_as_float(x[1])), sl2_2, nm2);
           const float2 xb = __ffma2_rn(make_float2(__uint_as_float(x[2]), __uint_as_float(x[3])), sl2_2, nm2);
           const float2 ea = make_float2(ex2(xa.x), ex2(xa.y));
-          const float2 eb = make_float2(ex2(xb.x), ex2(xb.y));
+          const float2 eb = kPoly && (c0 + c) % 8 == 4 ? exp2_fma(xb) : make_float2(ex2(xb.x), ex2(xb.y));
           s_a = __fadd2_rn(s_a, ea);
           s_b = __fadd2_rn(s_b, eb);
           sr[(c0 + c) / 2] = bits(__floats2half2_rn(ea.x, ea.y));
@@ -507,6 +536,7 @@ __device__ void softmax_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at
     if (!ok) { if (lane == 0) flag_timeout(sm, p); return; }
     // ---- O / l, or a piece's O and statistics
     tc_fence_after();
+    if (kPoly && !seen && l == l) l = 0.f;       // (the polynomial's least weight is 2^-126, also for what is hidden)
     if (!finite && seen) l = NAN;                // (a row that is not finite and sees something)
     const bool whole = at.begins() && at.ends();
     const Place to(p, at, s * kTileRows + row);  // (again: registers are scarce in between)

@@ -110,7 +110,8 @@ def norm_rope(x, weight, cos, sin, positions, eps, interleaved):
 def attention(q, cu, kv_lens, table, k, v, page_size, causal, scale, k_all_pages):
     """q [T, H, d]; k, v [slots, Hk, d] float64.  Returns out, lse, tolerance of out before its last rounding, tolerance of lse.
 
-    Error of a weight, relative: 2^-11 for its rounding to fp16; 2^-21 for exp2 and the subtraction's result; and the error of its
+    Error of a weight, relative: 2^-11 for its rounding to fp16; 2^-18 for exp2 (2.6e-6 of a polynomial, d = 64; the instruction 2^-21) and the
+    subtraction's result; and the error of its
     logit, d products of exact operands summed in fp32 with an error of 2^-23 of the partial sums at each step, the scaling
     (2^-23) and the subtraction of the maximum (2^-24 of its result, at most 2 largest logits).  Numerator and denominator both
     have the logits' error.  The sums over n keys in fp32: 2^-23 for each of the tree's n / 16 + 64 steps of its magnitude sum p |v|.
@@ -149,7 +150,7 @@ def attention(q, cu, kv_lens, table, k, v, page_size, causal, scale, k_all_pages
             logit = (size.amax(-1) if n else torch.zeros(m, dtype=torch.float64)) * (d + 8) * 2.0 ** -23
             wn = (w / torch.where(some, total, 1.0)[:, None]).nan_to_num(0)
             mass = wn @ vz.abs().nan_to_num(0)
-            tol[lo:hi, h] = mass * (2.0 ** -11 + 2.0 ** -20 + 2 * logit[:, None] + (n / 16 + 64) * 2.0 ** -23) + \
+            tol[lo:hi, h] = mass * (2.0 ** -11 + 2.0 ** -18 + 2 * logit[:, None] + (n / 16 + 64) * 2.0 ** -23) + \
                 n * 2.0 ** -36 * (vz.abs().nan_to_num(0).max() if n else 0)
-            tol_lse[lo:hi, h] = 2 * logit + (n / 16 + 80) * 2.0 ** -23 + 2.0 ** -22 * lse[lo:hi, h].abs().nan_to_num(0, 0, 0)
+            tol_lse[lo:hi, h] = 2.0 ** -18 + 2 * logit + (n / 16 + 80) * 2.0 ** -23 + 2.0 ** -22 * lse[lo:hi, h].abs().nan_to_num(0, 0, 0)
     return out, lse, tol, tol_lse, touched
