@@ -324,7 +324,7 @@ enum { SOL_TYPE_BF16 = 0, SOL_TYPE_FP16 = 1 };
  * loops has two of kv_lens / old_lens and of result / free_count, and swaps them.
  *
  * Pages are taken for the first max_blocks blocks of a request only.  More new tokens than max_tokens: those behind it have no
- * slot and are counted in result[1]. */
+ * slot and are counted in result[1]; their pages are taken and entered all the same. */
 typedef struct {
   const int32_t* old_lens; const int32_t* new_lens;
   const int32_t* free_pages; const int32_t* free_count;

@@ -70,10 +70,7 @@ def tables(old, new, free, count, table, page_size, max_tokens):
             j, slot = p // page_size, -1
             if j < len(table[b]):
                 if p % page_size == 0:
-                    page = stack.pop() if stack else -1
-                    if len(slots) < max_tokens:
-                        table[b][j] = page
-                    taken = page
+                    taken = table[b][j] = stack.pop() if stack else -1
                 else:
                     taken = table[b][j] if p == o or j == o // page_size else taken
                 if taken >= 0:
