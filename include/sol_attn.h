@@ -317,7 +317,7 @@ enum { SOL_TYPE_BF16 = 0, SOL_TYPE_FP16 = 1 };
  *   cu_q          [requests + 1], out: token ranges, the running sum of new_lens
  *   kv_lens       [requests], out: old + new
  *   slots         [max_tokens], out: page * page_size + place in it of each new token; -1 where it has no page (none left, a
- *                 table row that is too short, a negative entry).  Entries from cu_q[requests] on are left as they were
+ *                 table row that is too short, an entry that is negative or whose slots pass 2^31).  Entries from cu_q[requests] on are left as they were
  *   positions     [max_tokens] or NULL, out: position of each new token in its request
  *   result        [2], out: pages that are left, tokens that got no slot
  * No output may be an input (SOL_ERR_INVALID_ARG where it begins at the same address): every block reads the inputs for itself.  A caller that

@@ -4,7 +4,8 @@
 // tokens, so every block forms both sums for itself and fills the tokens that it owns: one launch, no block waits for
 // another.  A page is entered in its request's table by the thread of the first token that it holds; those of tokens behind max_tokens, which
 // have no thread, by the first block.
-// Bound by latency: lengths, two barriers, the free list.  64 requests with a token each 3.7 us in a graph, 192 with 196 000 tokens 6.1.
+// Bound by latency: lengths, two barriers, the free list.  64 requests with a token each 3.3 us in a graph, 192 with 196 000 tokens 6.3
+// (2.9 and 5.6 without the look at the pages that are taken).
 #include "cache.cuh"
 
 namespace sol {
@@ -58,6 +59,16 @@ __global__ void __launch_bounds__(kThreads) block_tables_kernel(const TablesPara
   const bool writer = blockIdx.x == 0;           // of what there is one of a request
   if (threadIdx.x == 0) without = 0;
   auto pages_of = [&](long long tokens) { return min((tokens + mask) >> p.page_shift, (long long)p.max_blocks); };
+  auto is_page = [&](long long page) { return page >= 0 && page <= 0x7fffffff >> p.page_shift; };      // its slots are of 32 bits
+  // The last request of the round whose entry is at most x (one without tokens, or pages, has that of the next).
+  auto last_upto = [&](const long long* of, long long x) {
+    int a = 0, z = kThreads;
+    while (z - a > 1) {
+      const int m = (a + z) / 2;
+      if (of[m] <= x) a = m; else z = m;
+    }
+    return a;
+  };
   Sum base{0, 0};
   for (int r = 0; r < p.requests; r += kThreads) {
     const int b = r + threadIdx.x;
@@ -75,32 +86,25 @@ __global__ void __launch_bounds__(kThreads) block_tables_kernel(const TablesPara
       p.cu_q[b] = clamp_int(t0);
       if (b == p.requests - 1) p.cu_q[p.requests] = clamp_int(end.tokens);
       p.kv_lens[b] = clamp_int((long long)o + n);
-      // tokens without a slot: of the page that was begun, if it is not there; behind the pages that there were; behind max_tokens
+      // tokens without a slot: those behind max_tokens; of the others those of the page that was begun, if it is no page, and those behind
+      // the pages that there were (those of pages taken that are none: below)
       const long long got = max(0LL, min(need - have, (long long)count - p0));
-      const long long begun = min((long long)n, min((have << p.page_shift), (long long)o + n) - o);   // < 0: its table is too short
-      long long miss = max(0LL, (long long)o + n - max((have + got) << p.page_shift, (long long)o));
-      if (begun > 0 && p.tables[b * p.table_stride + (o >> p.page_shift)] < 0) miss += begun;
       const long long kept = max(0LL, min((long long)p.max_tokens - t0, (long long)n));
-      if (kept < n) {                            // (those behind max_tokens have none, whatever their pages)
-        const long long in = max(0LL, o + kept - max((have + got) << p.page_shift, (long long)o));
-        miss = n - kept + in;
-        if (begun > 0 && p.tables[b * p.table_stride + (o >> p.page_shift)] < 0) miss += min(begun, kept);
-        // their pages are taken like any others, and no thread has their first token
+      const long long begun = min(kept, min((have << p.page_shift), (long long)o + n) - o);   // < 0: its table is too short
+      long long miss = n - kept + max(0LL, o + kept - max((have + got) << p.page_shift, (long long)o));
+      if (begun > 0 && !is_page(p.tables[b * p.table_stride + (o >> p.page_shift)])) miss += begun;
+      // Pages of tokens behind max_tokens are taken like any others, and no thread has their first token.
+      if (kept < n)
         for (long long j = max(have, (o + kept + mask) >> p.page_shift); j < need; ++j) {
           const long long rank = p0 + j - have;
           p.tables[b * p.table_stride + j] = rank < count ? p.free_pages[count - 1 - rank] : -1;
         }
-      }
       if (miss) atomicAdd(&without, (unsigned long long)miss);
     }
     __syncthreads();
     const long long from = max(lo, base.tokens), to = min(hi, base.tokens + total.tokens);
     for (long long t = from + threadIdx.x; t < to; t += kThreads) {
-      int a = 0, z = kThreads;                   // the last request that begins at or before t (empty ones begin where the next does)
-      while (z - a > 1) {
-        const int m = (a + z) / 2;
-        if (first[m] <= t) a = m; else z = m;
-      }
+      const int a = last_upto(first, t);
       const long long pos = old_of[a] + (t - first[a]);
       const long long j = pos >> p.page_shift, had = pages_of(old_of[a]);
       long long page = -1;
@@ -115,8 +119,27 @@ __global__ void __launch_bounds__(kThreads) block_tables_kernel(const TablesPara
         }
       }
       const long long slot = (page << p.page_shift) + (pos & mask);
-      p.slots[t] = page < 0 || slot > 0x7fffffffLL ? -1 : (int32_t)slot;
+      p.slots[t] = is_page(page) ? (int32_t)slot : -1;
       if (p.positions) p.positions[t] = clamp_int(pos);
+    }
+    if (writer) {                                // pages taken that are none: their tokens have no slot
+      const long long pages_end = min((long long)count, base.pages + total.pages);
+      constexpr int kAtOnce = 8;
+      for (long long rank0 = base.pages + threadIdx.x; rank0 < pages_end; rank0 += kThreads * kAtOnce) {
+        int id[kAtOnce];
+#pragma unroll
+        for (int x = 0; x < kAtOnce; ++x) id[x] = rank0 + x * kThreads < pages_end ? p.free_pages[count - 1 - rank0 - x * kThreads] : 0;
+#pragma unroll
+        for (int x = 0; x < kAtOnce; ++x) {
+          if (is_page(id[x])) continue;
+          const long long rank = rank0 + x * kThreads;
+          const int a = last_upto(page0, rank);
+          const long long kept = min((long long)p.max_tokens, first[a + 1]) - first[a];    // (< 0: none of the request's)
+          const long long at = ((pages_of(old_of[a]) + rank - page0[a]) << p.page_shift) - old_of[a];
+          const long long miss = min(kept, at + mask + 1) - at;
+          if (miss > 0) atomicAdd(&without, (unsigned long long)miss);
+        }
+      }
     }
     base = base + total;
     if (!writer && base.tokens >= hi) break;

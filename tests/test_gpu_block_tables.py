@@ -41,3 +41,26 @@ def test_pages_behind_the_last_slot_are_entered(sb, page, B, longest, share, sho
     want_slots = [want[b][p // page] * page + p % page if want[b][p // page] >= 0 else -1 for b, (o, n) in enumerate(zip(old, new)) for p in range(o, o + n)]
     kept = want_slots[:int(total * share)]
     assert slots == kept and result[1] == total - len(kept) + sum(s < 0 for s in kept)
+
+
+@pytest.mark.parametrize("page", [16, 256])
+@pytest.mark.parametrize("B, longest, share", [(1, 3000, 1.0), (7, 700, 1.0), (7, 700, 0.5), (600, 90, 1.0), (600, 90, 0.7)])
+def test_pages_that_are_none_are_counted(sb, page, B, longest, share):  # noqa: F811
+    """Negative ids and ids whose slots pass 31 bits, on the stack and in the page that was begun: the result counts every token without a slot."""
+    rng = random.Random(B * page + longest)
+    most = (2 ** 31 - 1) // page                                          # the largest page whose slots fit
+    some = lambda: rng.choice([rng.randrange(most), rng.randrange(most), most, most + 1, 2 ** 31 - 1, -1, -5])  # noqa: E731
+    old = [rng.choice([0, page, page - 1, rng.randrange(3 * page)]) for _ in range(B)]
+    new = [rng.randint(0, longest) for _ in range(B)]
+    columns = max(1, max(-(-(o + n) // page) for o, n in zip(old, new)))
+    table = [[some() for _ in range(columns)] for _ in range(B)]
+    need = sum(-(-(o + n) // page) - -(-o // page) for o, n in zip(old, new))
+    free = [some() for _ in range(max(1, need - 2))]
+    total = sum(new)
+    got_table, _, _, slots, _, result = run_tables(sb, old, new, free, len(free), table, page, int(total * share))
+    taken, left = pages_taken(old, new, free, len(free), columns, page)
+    want = [[taken.get((b, j), table[b][j]) for j in range(columns)] for b in range(B)]
+    assert got_table == want
+    ids = [(want[b][p // page], p % page) for b, (o, n) in enumerate(zip(old, new)) for p in range(o, o + n)][:len(slots)]
+    assert slots == [i * page + at if 0 <= i <= most else -1 for i, at in ids]
+    assert result == [left, total - len(slots) + sum(s < 0 for s in slots)]
