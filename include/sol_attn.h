@@ -396,7 +396,8 @@ sol_status_t sol_attn_cache_read(const sol_attn_cache* cache /* host */, void* k
 
 /* Softmax attention of a ragged batch of queries over the cache.  Request b has the queries q[cu_q[b]] ... q[cu_q[b + 1] - 1] and the
  * first kv_lens[b] tokens of its block table (clamped to max_blocks * page_size).  With `causal`, query i of n sees the first
- * kv_len - n + i + 1 tokens, else all.  Query head h uses key / value head h / (Hq / Hk).
+ * kv_len - n + i + 1 tokens, else all (n and kv_len as they are given, also where cu_q passes `tokens` or kv_lens the table: each query
+ * keeps its place).  Query head h uses key / value head h / (Hq / Hk).
  *
  *   q, out       [tokens][Hq][d], element strides {token, head}, multiples of 8; rows outside the requests are neither read nor written; out may not
  *                be q (SOL_ERR_INVALID_ARG)

@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
 #pragma unroll
         for (int j = 0; j < 2; ++j) qf[nb][s][j] = bits(__floats2half2_rn(x[4 * s + 2 * j] * up, x[4 * s + 2 * j + 1] * up));
       const float mine2 = finite ? p.sl2 / up : NAN;             // a row that is not finite gives NaN
-      const int seen = !on ? 0 : p.causal ? max(0, r.keys - r.queries + qi + 1) : r.keys;
+      const int seen = !on ? 0 : p.causal ? r.sees(qi) : r.keys;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         sl2[nb][j] = __shfl_sync(kAll, mine2, (2 * t + j) * 4);

@@ -43,14 +43,21 @@ struct AttnParams {
   float* parts;                                  // two partial results per block
 };
 
-// Queries and keys of a request, within what the caller's buffers hold.
-struct Request { int first, queries, keys; };
+// Queries and keys of a request, within what the caller's buffers hold.  What they do not hold still has its place: query i lies `ahead` + i
+// behind the request's first key also where the last queries are not in q, or the last keys not in the table.
+struct Request {
+  int first, queries, keys, ahead;
+  __device__ int sees(int i) const { return (int)max(0LL, min((long long)keys, (long long)ahead + i + 1)); }     // keys that query i sees, causal
+};
 __device__ __forceinline__ Request request_at(const AttnParams& p, int b) {
+  const int end = p.cu_q[b + 1];
+  const long long kv = max(0, p.kv_lens[b]);
   Request r;
   r.first = max(0, min(p.cu_q[b], p.tokens));
-  r.queries = max(0, min(p.cu_q[b + 1], p.tokens) - r.first);
+  r.queries = max(0, min(end, p.tokens) - r.first);
   // (0x7fff0000: sums with a step stay within 32 bits; a cache has fewer tokens than 2^31)
-  r.keys = (int)max(0LL, min(min((long long)p.kv_lens[b], (long long)p.max_blocks << p.page_shift), 0x7fff0000LL));
+  r.keys = (int)min(min(kv, (long long)p.max_blocks << p.page_shift), 0x7fff0000LL);
+  r.ahead = (int)max(-0x7fffffffLL, min(kv - end + r.first, (long long)r.keys));
   return r;
 }
 
@@ -71,7 +78,7 @@ struct Tiles {
     int sees = r.keys;
     if (p.causal) {
       const int last = min((tile + 1) * kRows, r.queries * p.group) - 1;
-      sees = min(sees, r.keys - r.queries + last / p.group + 1);
+      sees = r.sees(last / p.group);
     }
     return max(1, (sees + kStep - 1) / kStep);
   }
@@ -152,9 +159,9 @@ template <int kThreads, class Tiling>
 __device__ Shares find_share(const AttnParams& p, long long c, long long* sums, Start* start) {
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
   long long all = 0, x = 0, n = 0;
-  Request r{0, 0, 0};
+  Request r{0, 0, 0, 0};
   auto scan = [&](int b0) {                      // of requests b0 ...: x the sum up to this thread's, n its own; returns that of all
-    r = Request{0, 0, 0};
+    r = Request{0, 0, 0, 0};
     n = 0;
     if (b0 + tid < p.requests) { r = request_at(p, b0 + tid); n = Tiling::per_head(p, r) * p.Hk; }
     x = n;

@@ -389,7 +389,7 @@ __device__ void softmax_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at
     if (s >= tiles_of(p, at)) continue;
     const Place at_row(p, at, s * kTileRows + row);
     // (a row that is not there sees all: it would have every tile masked)
-    const int sees = at_row.on && p.causal ? min(at.r.keys, max(0, at.r.keys - at.r.queries + at_row.query + 1)) : at.r.keys;
+    const int sees = at_row.on && p.causal ? at.r.sees(at_row.query) : at.r.keys;
     // ---- the row's queries, scaled by a power of two: the largest becomes 2^14 to 2^15 (see cache_attention.cu)
     float sl2;
     bool finite = true;
