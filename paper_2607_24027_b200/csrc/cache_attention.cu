@@ -364,7 +364,9 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
       if (!__all_sync(kAll, mbar_wait(&sh.full[s], (n / kStages) & 1, &sh.abort_flag, p.wait_limit))) { ok = false; break; }
       const unsigned char* stage = smem + s * C::kStageBytes + warp * 2 * U::kBytes;
       const int key0 = step * kStep + warp * kWarpKeys;
-      if (key0 + kWarpKeys <= least && !*(volatile int*)&sh.missing) work_on(step, stage, std::true_type{});
+      // (a vote: another warp may be setting the word, and what follows is for whole warps)
+      const bool missing = __any_sync(kAll, *(volatile int*)&sh.missing != 0);
+      if (key0 + kWarpKeys <= least && !missing) work_on(step, stage, std::true_type{});
       else if (key0 < r.keys) work_on(step, stage, std::false_type{});
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.empty[s]);

@@ -438,7 +438,8 @@ __device__ void softmax_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at
       tc_fence_after();
       // Columns that the row does not see are set to -inf where they lie, 16 at a time: this is rare, and as code between the loads and the
       // maxima it pushed the common path out of the instruction cache (2.63 us a step, 2.09 without it)
-      const bool missing = *(volatile int*)&sm.missing != 0;
+      // (a vote: the loader may be setting the word, and the TMEM accesses are for whole warps)
+      const bool missing = __any_sync(kAll, *(volatile int*)&sm.missing != 0);
       if (__any_sync(kAll, left < kCols) || missing) {
 #pragma unroll 1
         for (int x = 0; x < kUnits; ++x) {

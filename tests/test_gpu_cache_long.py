@@ -1,0 +1,85 @@
+"""Attention over the cache in the state in which long calls run: blocks with ten steps and more, rings that have turned, several pieces."""
+import math
+import random
+
+import pytest
+import torch
+
+from tests import cache_reference as ref
+from tests.test_gpu_cache import batch, filled, ints, sb  # noqa: F401  (sb: a fixture)
+
+pytestmark = pytest.mark.gpu
+SMS = 148
+FEW, FEW_WIDE, MANY = 4 * SMS, 3 * SMS, SMS                               # blocks: up to 8 rows, up to 48 rows, more
+# kind: (requests as (keys, queries), Hq, Hk), 10 or more steps to a block
+CALLS = {
+    "tokens": ([(70001, 1)], 32, 16),
+    "tokens, ragged": ([(60000, 1), (9, 1), (50111, 1), (0, 1), (9000, 1), (127, 1)], 16, 8),
+    "drafts": ([(33000, 5), (20007, 3)], 16, 16),
+    "drafts, wide": ([(30000, 4), (21000, 1)], 40, 8),
+    "chunks": ([(8000, 300)], 40, 40),
+    "chunks, ragged": ([(6001, 300), (20, 20), (5000, 130), (3000, 1), (2999, 700)], 32, 16),
+}
+
+
+def values_of(sb, cache):  # noqa: F811
+    """What every slot holds, read back (exact in 16 bits; that reading is right is tested by the bytes)."""
+    n, dt = cache.pages * cache.page_size, torch.bfloat16
+    k, v = (torch.empty(n, cache.heads, cache.d, dtype=dt, device="cuda") for _ in range(2))
+    sb.sol_attn_cache_read(cache, torch.arange(n, dtype=torch.int32, device="cuda"), k, v)
+    return k.double(), v.double()
+
+
+def steps_of_a_block(requests, H, Hk):
+    """Steps that the block with the fewest has in the kernel for the most rows, from the header comments of the kernels."""
+    rows = max(n for _, n in requests) * (H // Hk)
+    tile, blocks = (8, FEW) if rows <= 8 else (16, FEW_WIDE) if rows <= 48 else (256, MANY)
+    total = 0
+    for kv, n in requests:
+        r = n * (H // Hk)
+        if rows <= 48 or r > 48 or len(requests) == 1:
+            total += Hk * sum(max(1, -(-max(1, kv - n + (min((i + 1) * tile, r) - 1) // (H // Hk) + 1) // 128)) for i in range(-(-r // tile)))
+    return total // blocks
+
+
+def check(sb, cache, q, cu, kv, table, causal=True, twice=True, workspace=None):  # noqa: F811
+    """Against the definition in 64 bits on the GPU; the same bits twice."""
+    k, v = values_of(sb, cache)
+    most = max(b - a for a, b in zip(cu, cu[1:]))
+    ws = sb.make_cache_workspace(most, q.shape[1], cache.heads, cache.d) if workspace is None else workspace
+    args = ints(cu), ints(kv), ints(table)
+    runs = []
+    for _ in range(2 if twice else 1):
+        out, lse = torch.full_like(q, 9.0), torch.full(q.shape[:2], 9.0, device="cuda")
+        sb.sol_attn_cache_attention(q, *args, cache, out, most, ws, lse=lse, causal=causal)
+        assert sb.sol_attn_cache_read_status(ws) == sb.SOL_OK
+        runs.append((out, lse))
+    if twice:
+        assert torch.equal(runs[0][0], runs[1][0]) and torch.equal(runs[0][1], runs[1][1])
+    with torch.device("cuda"):
+        want, want_lse, tol, tol_lse, _ = ref.attention(q, cu, kv, table, k, v, cache.page_size, causal, q.shape[2] ** -0.5, cache.pages)
+    bound = tol + ref.half_step(q.dtype) * (want.abs() + tol) + (2.0 ** -25 if q.dtype == torch.float16 else 0)
+    off = ((out.double() - want).abs() / bound).max().item()
+    assert off <= 1, off
+    assert torch.equal(lse.isinf(), want_lse.isinf())
+    some = ~want_lse.isinf()
+    off = ((lse.double() - want_lse).abs() / tol_lse)[some].max().item()
+    assert off <= 1, off
+    return out
+
+
+@pytest.mark.parametrize("d, dtype", [(128, torch.bfloat16), (64, torch.float16)])
+@pytest.mark.parametrize("kind", ["tokens", "drafts", "chunks"])
+def test_missing_pages_amid_long_pieces(sb, kind, d, dtype):  # noqa: F811
+    """Some pages are not there, found by a block at any of its steps while its other warps are at work."""
+    requests, H, Hk = CALLS[kind]
+    kv, new = [r[0] for r in requests], [r[1] for r in requests]
+    table, cu, pages = batch(kv, new, 64, 5)
+    rng = random.Random(8)
+    for row in table:
+        for j in range(0, len(row), 40):
+            row[rng.randrange(j, min(j + 40, len(row)))] = rng.choice([-1, pages, 2 ** 31 - 1, -2 ** 31])
+    cache = filled(sb, pages, 64, Hk, d, 3)
+    q = torch.randn(cu[-1], H, d, generator=torch.Generator().manual_seed(9)).to(dtype).cuda()
+    assert steps_of_a_block(requests, H, Hk) >= 10
+    check(sb, cache, q, cu, kv, table)
