@@ -29,6 +29,7 @@ constexpr int kWarpKeys = 32, kStep = kWarps * kWarpKeys;
 constexpr int kStages = 3;
 constexpr unsigned kAll = 0xffffffffu;
 constexpr int kBlocksPerSm = 4;
+constexpr long long kLanding = 1 << 20;          // SM clocks that a copy is given to land after a wait has run out, however short the limit
 constexpr long long kAnyRows = 1LL << 40;
 // Requests of up to so many rows (queries times the query heads of a key / value head) are this kernel's.  It takes as long as it has
 // tiles of 16 rows, the other as long for 20 as for 128.  us, this kernel / the other: 16 requests of 8192 keys on 8 heads, 20 rows 93 / 144,
@@ -381,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 4 : 3) cache_attention_ker
     if (sh.abort_flag) {                         // a wait ran out: no result, but no copy is left in flight either
       int never = 0;
       if (!ok)
-        for (uint32_t x = n; x < n + kStages; ++x) mbar_wait(&sh.full[x % kStages], (x / kStages) & 1, &never, p.wait_limit);
+        for (uint32_t x = n; x < n + kStages; ++x) mbar_wait(&sh.full[x % kStages], (x / kStages) & 1, &never, max(p.wait_limit, kLanding));
       if (tid == 0) p.records[blockIdx.x] = Record::none();
       return;
     }

@@ -58,7 +58,7 @@ struct Shared {
   uint64_t s_full[2];                            // scores of a tile are in TMEM
   uint64_t p_full[2][2];                         // first / second half of the columns of P are in TMEM
   uint64_t o_full[2], o_free[2];                 // accumulator complete / read
-  uint64_t mma_drain;                            // abort path only
+  uint64_t mma_drain;                            // everything that was issued is done
   long long sums[kThreads / 32];
   Start start;
   Pieces<Tiling> pieces[kThreads / 32];          // each warp's place in the block's share: registers are scarce
@@ -149,6 +149,7 @@ __device__ void loader_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at,
   using U = Unit<D>;
   const uint32_t unit_mask = (1u << (p.page_shift - 4)) - 1, head_bytes = (uint32_t)U::kBytes << (p.page_shift - 4);
   uint32_t n = lane;                             // this lane's unit, counted over all pieces
+  uint32_t asked = 0;                            // units that it has asked for: lane, lane + kUnits, ...
   bool ok = true;
   while (ok && next_piece(at, p, lane)) {
     const int32_t* table = p.tables + at.b * p.table_stride;
@@ -168,6 +169,7 @@ __device__ void loader_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at,
           const uint32_t slot = n % kRaw;
           mine = WAIT_CALL(&sm.raw_empty[slot], ((n / kRaw) & 1) ^ 1);
           if (mine) {
+            ++asked;
             int valid = max(0, min(keys - u * kUnit, kUnit));
             if (valid > 0 && (page < 0 || page >= p.pages)) { *(volatile int*)&sm.missing = 1; valid = 0; }
             *(volatile int*)&sm.raw_valid[slot] = valid;
@@ -183,17 +185,18 @@ __device__ void loader_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at,
       page = next_page;
     }
   }
-  if (!ok) {
-    if (lane == 0) flag_timeout(sm, p);
-    // let copies that are still in flight land before the block's shared memory goes away (not cut short by the flag)
-    int never = 0;
-    if (lane < kUnits)
-      for (int back = 1; back <= 2 && n >= (uint32_t)(back * kUnits); ++back) {
-        const uint32_t x = n - back * kUnits;
-        mbar_wait_inline(&sm.raw_full[x % kRaw], (x / kRaw) & 1, &never, p.wait_limit);
-      }
-  }
+  if (!ok && lane == 0) flag_timeout(sm, p);
+  // The block's shared memory must not go away under a copy, whoever ended the block and why: wait (bounded, not cut short by the flag) for
+  // the last units of each lane, but for those whose place in the ring has been given to a later one (their barrier is a phase further).
+  const uint32_t next = __shfl_sync(kAll, asked, (lane + kRaw) % kUnits);
+  int never = 0;
+  if (lane < kUnits)
+    for (uint32_t back = 1; back <= 2 && back <= asked; ++back) {
+      const uint32_t x = lane + (asked - back) * kUnits;
+      if ((x + kRaw) / kUnits >= next) mbar_wait(&sm.raw_full[x % kRaw], (x / kRaw) & 1, &never);
+    }
 }
+static_assert(kRaw <= 2 * kUnits, "a lane's last two units are all that can be on their way");
 
 // Raw units to fp16 tiles.  The tasks, eight units of keys and eight of values for each tile of keys, lie one after the other, and
 // kWideners warps take them in turn.
@@ -365,12 +368,11 @@ __device__ void mma_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at, un
 #undef NEED
   if (!ok && leader) flag_timeout(sm, p);
   __syncwarp();
-  if (sm.abort_flag) {
-    // TMEM must not be released while MMAs are still writing to it: wait (bounded) behind everything issued
-    if (leader) mma_commit(&sm.mma_drain);
-    int never = 0;
-    mbar_wait_inline(&sm.mma_drain, 0, &never, p.wait_limit);
-  }
+  // TMEM must not be released, nor shared memory go away, while MMAs use them: wait (bounded) behind everything that was issued, also if it is
+  // another role that gives up, before or after this.
+  if (leader) mma_commit(&sm.mma_drain);
+  int never = 0;
+  mbar_wait(&sm.mma_drain, 0, &never);
 }
 
 template <class T, int D>

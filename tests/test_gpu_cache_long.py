@@ -59,12 +59,12 @@ def check(sb, cache, q, cu, kv, table, causal=True, twice=True, workspace=None):
     with torch.device("cuda"):
         want, want_lse, tol, tol_lse, _ = ref.attention(q, cu, kv, table, k, v, cache.page_size, causal, q.shape[2] ** -0.5, cache.pages)
     bound = tol + ref.half_step(q.dtype) * (want.abs() + tol) + (2.0 ** -25 if q.dtype == torch.float16 else 0)
-    off = ((out.double() - want).abs() / bound).max().item()
-    assert off <= 1, off
+    error = (out.double() - want).abs()
+    assert (error <= bound).all(), (error / bound).nan_to_num(0).max().item()          # (a query without keys: both are 0)
     assert torch.equal(lse.isinf(), want_lse.isinf())
     some = ~want_lse.isinf()
-    off = ((lse.double() - want_lse).abs() / tol_lse)[some].max().item()
-    assert off <= 1, off
+    error, bound = (lse.double() - want_lse)[some].abs(), tol_lse[some]
+    assert (error <= bound).all(), (error / bound).max().item()
     return out
 
 
@@ -83,3 +83,26 @@ def test_missing_pages_amid_long_pieces(sb, kind, d, dtype):  # noqa: F811
     q = torch.randn(cu[-1], H, d, generator=torch.Generator().manual_seed(9)).to(dtype).cuda()
     assert steps_of_a_block(requests, H, Hk) >= 10
     check(sb, cache, q, cu, kv, table)
+
+
+@pytest.mark.parametrize("kind", list(CALLS))
+@pytest.mark.parametrize("withheld", [5, 8, 10])
+def test_a_wait_that_runs_out_late(sb, kind, withheld):  # noqa: F811
+    """The arrival that is left out is that of a step behind the rings' first turn, with copies and products under way."""
+    requests, H, Hk = CALLS[kind]
+    kv, new = [r[0] for r in requests], [r[1] for r in requests]
+    table, cu, pages = batch(kv, new, 64, 5)
+    cache = filled(sb, pages, 64, Hk, 128, 3)
+    q = torch.randn(cu[-1], H, 128, generator=torch.Generator().manual_seed(9)).bfloat16().cuda()
+    ws, out = sb.make_cache_workspace(max(new), H, Hk, 128), torch.empty_like(q)
+    assert steps_of_a_block(requests, H, Hk) > withheld // (2 if max(new) > 48 else 1)
+    for limit in (200_000, 1):
+        sb.sol_attn_debug_set_wait(limit, withheld)
+        try:
+            sb.sol_attn_cache_attention(q, ints(cu), ints(kv), ints(table), cache, out, max(new), ws)
+            torch.cuda.synchronize()
+        finally:
+            sb.sol_attn_debug_set_wait()
+        assert sb.sol_attn_cache_read_status(ws) == sb.SOL_ERR_DEVICE_TIMEOUT
+        assert sb.sol_attn_cache_read_status(ws) == sb.SOL_OK
+    check(sb, cache, q, cu, kv, table, workspace=ws)
