@@ -342,7 +342,7 @@ sol_status_t sol_attn_block_tables(const sol_attn_tables_args* args /* host */);
  *
  *   q, k, q_out, k_out   [batch][tokens][heads][d] in any order of the first three, given by the element strides {batch, token,
  *                        head} of each; d channels contiguous, strides multiples of 8.  q_out may be q and k_out k, with the same
- *                        strides.  k may be NULL with Hk = 0 (or q with Hq = 0)
+ *                        strides (SOL_ERR_INVALID_ARG with others).  k may be NULL with Hk = 0 (or q with Hq = 0)
  *   q_weight, k_weight   fp32 [d], or NULL for ones
  *   cos, sin             fp32 [table_rows][rot / 2]; not read when rot = 0
  *   positions            int32 [batch][tokens]; NULL: the index of the token in its batch.  A token whose position is not in

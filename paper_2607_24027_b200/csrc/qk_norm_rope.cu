@@ -138,6 +138,13 @@ extern "C" sol_status_t sol_attn_qk_norm_rope(const sol_attn_norm_args* a) {
   if (!sol::cache::strides_ok(a->q_stride, a->Hq ? B : 0, a->Hq ? N : 0, a->Hq) || !sol::cache::strides_ok(a->q_out_stride, a->Hq ? B : 0, a->Hq ? N : 0, a->Hq) ||
       !sol::cache::strides_ok(a->k_stride, a->Hk ? B : 0, a->Hk ? N : 0, a->Hk) || !sol::cache::strides_ok(a->k_out_stride, a->Hk ? B : 0, a->Hk ? N : 0, a->Hk))
     return SOL_ERR_INVALID_ARG;
+  // In place each head lies where it lay; another order, or the other tensor's place, would be written while warps still read it.
+  auto lies_as = [&](const void* in, const void* out, const int64_t* si, const int64_t* so, int H) {
+    return in != out || ((B <= 1 || si[0] == so[0]) && (N <= 1 || si[1] == so[1]) && (H <= 1 || si[2] == so[2]));
+  };
+  if (a->Hq && !lies_as(a->q, a->q_out, a->q_stride, a->q_out_stride, a->Hq)) return SOL_ERR_INVALID_ARG;
+  if (a->Hk && !lies_as(a->k, a->k_out, a->k_stride, a->k_out_stride, a->Hk)) return SOL_ERR_INVALID_ARG;
+  if (a->Hq && a->Hk && (a->q_out == a->k || a->k_out == a->q || a->q_out == a->k_out)) return SOL_ERR_INVALID_ARG;
   const sol_status_t s = sol::check_device_arch();
   if (s != SOL_OK) return s;
   int dev = 0, sms = 0;
