@@ -302,7 +302,8 @@ sol_status_t sol_attn_route_materialized(const float* qbar, const float* kc, int
  * programmatic stream serialization like the kernels above.  (The paper has no counterpart: its kernels see whole sequences.)
  * Index arrays are int32 and 4-byte aligned, everything else 16-byte aligned; strides are in elements
  * (that of a dimension of one is not looked at); the device pointers
- * belong to the current device, `stream` too.  Outputs must not overlap inputs or one another unless an entry says so. */
+ * belong to the current device, `stream` too.  Outputs must not overlap inputs or one another unless an entry says so, nor
+ * rows of an output each other (a stride of 0 there is SOL_ERR_INVALID_ARG). */
 
 /* 16-bit element types of the entry points below */
 enum { SOL_TYPE_BF16 = 0, SOL_TYPE_FP16 = 1 };

@@ -55,6 +55,8 @@ inline bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr
 inline bool strides_ok(const int64_t* s, int a, int b, int c = 1) {
   return (a <= 1 || s[0] % 8 == 0) && (b <= 1 || s[1] % 8 == 0) && (c <= 1 || s[2] % 8 == 0);
 }
+// Rows of an output do not lie on one another (as those of an expanded tensor do).
+inline bool rows_apart(const int64_t* s, int a, int b, int c = 1) { return (a <= 1 || s[0]) && (b <= 1 || s[1]) && (c <= 1 || s[2]); }
 
 #ifdef __CUDACC__
 // Where a slot's unit of a head starts.

@@ -707,6 +707,7 @@ sol_status_t check_attention(const sol_attn_cache_args* a) {
   if (a->tokens > 0 && a->q == a->out) return SOL_ERR_INVALID_ARG;             // several blocks read a row's queries
   if (a->tokens > 0 && (!a->q || !a->out || !aligned(a->q, 16) || !aligned(a->out, 16))) return SOL_ERR_INVALID_ARG;
   if (!strides_ok(a->q_stride, a->tokens, a->Hq) || !strides_ok(a->out_stride, a->tokens, a->Hq) || !aligned(a->lse, 4)) return SOL_ERR_INVALID_ARG;
+  if (!rows_apart(a->out_stride, a->tokens, a->Hq)) return SOL_ERR_INVALID_ARG;
   if (a->requests > 0 && (!a->cu_q || !a->kv_lens || !a->block_tables)) return SOL_ERR_INVALID_ARG;
   if (!aligned(a->cu_q, 4) || !aligned(a->kv_lens, 4) || !aligned(a->block_tables, 4)) return SOL_ERR_INVALID_ARG;
   const size_t need = sol_attn_cache_workspace_bytes(a->max_q, a->Hq, a->cache.Hk, a->cache.d);

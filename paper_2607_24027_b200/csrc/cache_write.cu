@@ -218,6 +218,7 @@ sol_status_t launch(int what, const sol_attn_cache* c, const void* k, const void
     const void* x = i ? v : k;
     const int64_t* st = i ? vs : ks;
     if (x && (!st || !cache::aligned(x, 16) || !cache::strides_ok(st, tokens, c->Hk))) return SOL_ERR_INVALID_ARG;
+    if (x && what == kRead && !cache::rows_apart(st, tokens, c->Hk)) return SOL_ERR_INVALID_ARG;
   }
   if (!slots || !cache::aligned(slots, 4)) return SOL_ERR_INVALID_ARG;
   if ((s = check_device_arch()) != SOL_OK) return s;

@@ -142,6 +142,8 @@ extern "C" sol_status_t sol_attn_qk_norm_rope(const sol_attn_norm_args* a) {
   auto lies_as = [&](const void* in, const void* out, const int64_t* si, const int64_t* so, int H) {
     return in != out || ((B <= 1 || si[0] == so[0]) && (N <= 1 || si[1] == so[1]) && (H <= 1 || si[2] == so[2]));
   };
+  if ((a->Hq && !sol::cache::rows_apart(a->q_out_stride, B, N, a->Hq)) || (a->Hk && !sol::cache::rows_apart(a->k_out_stride, B, N, a->Hk)))
+    return SOL_ERR_INVALID_ARG;
   if (a->Hq && !lies_as(a->q, a->q_out, a->q_stride, a->q_out_stride, a->Hq)) return SOL_ERR_INVALID_ARG;
   if (a->Hk && !lies_as(a->k, a->k_out, a->k_stride, a->k_out_stride, a->Hk)) return SOL_ERR_INVALID_ARG;
   if (a->Hq && a->Hk && (a->q_out == a->k || a->k_out == a->q || a->q_out == a->k_out)) return SOL_ERR_INVALID_ARG;

@@ -3,7 +3,7 @@ import ctypes
 
 import pytest
 
-from tests.test_cache_host import norm_args, sb  # noqa: F401  (sb: a fixture)
+from tests.test_cache_host import P, attention_args, cache_of, norm_args, sb  # noqa: F401  (sb: a fixture)
 
 two, three = ctypes.c_int64 * 2, ctypes.c_int64 * 3
 
@@ -14,3 +14,17 @@ two, three = ctypes.c_int64 * 2, ctypes.c_int64 * 3
 def test_norm_in_place_with_other_strides_or_the_others_place(sb, change):  # noqa: F811
     """q_out may be q with q's strides and k_out k, but neither the other's input or output: warps read and write heads on their own."""
     assert sb.lib().sol_attn_qk_norm_rope(ctypes.byref(norm_args(sb, **change))) == sb.SOL_ERR_INVALID_ARG
+
+
+def test_outputs_whose_rows_lie_on_one_another(sb):  # noqa: F811
+    """Strides of 0, as of an expanded tensor, of a dimension with more than one entry; inputs may have them."""
+    bad, c = sb.SOL_ERR_INVALID_ARG, cache_of(sb)
+    for st in (two(0, 128), two(512, 0)):
+        assert sb.lib().sol_attn_cache_attention(ctypes.byref(attention_args(sb, out_stride=st))) == bad
+        assert sb.lib().sol_attn_cache_read(ctypes.byref(c), P(4096), P(1 << 20), st, two(256, 128), P(4096), 4, 0, None) == bad
+        assert sb.lib().sol_attn_cache_read(ctypes.byref(c), None, P(1 << 20), None, st, P(4096), 4, 0, None) == bad
+    for st in (three(0, 512, 128), three(4096, 0, 128), three(4096, 512, 0)):
+        for side in ("q", "k"):
+            for where in (4096 if side == "q" else 8192, 1 << 20):
+                a = norm_args(sb, batch=2, **{side + "_out": where, side + "_stride": st, side + "_out_stride": st})
+                assert sb.lib().sol_attn_qk_norm_rope(ctypes.byref(a)) == bad
