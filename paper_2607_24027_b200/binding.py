@@ -497,12 +497,18 @@ class Cache:
     v_exp: int = 0
 
     def __post_init__(self):
-        self.bytes = sol_attn_cache_bytes(self.pages, self.page_size, self.heads, self.d)
+        self._sized()
+
+    def _sized(self):
+        self._shape = self.pages, self.page_size, self.heads, self.d
+        self.bytes = sol_attn_cache_bytes(*self._shape)
         if self.bytes == 0:
             raise SolAttnError(SOL_ERR_UNSUPPORTED_SHAPE, "sol_attn_cache_bytes")
 
     def c(self, dev: int):
         """The members of ``sol_attn_cache``."""
+        if self._shape != (self.pages, self.page_size, self.heads, self.d):      # (they may have been changed since)
+            self._sized()
         t = self.data
         if t.dtype is not _U8 or t.get_device() != dev or not t.is_contiguous() or t.numel() < self.bytes:
             raise ValueError(f"cache: expected a contiguous uint8 tensor of {self.bytes} bytes on the current CUDA device")

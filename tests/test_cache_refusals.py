@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 from tests.test_cache_host import P, attention_args, cache_of, norm_args, sb  # noqa: F401  (sb: a fixture)
 
@@ -28,3 +29,19 @@ def test_outputs_whose_rows_lie_on_one_another(sb):  # noqa: F811
             for where in (4096 if side == "q" else 8192, 1 << 20):
                 a = norm_args(sb, batch=2, **{side + "_out": where, side + "_stride": st, side + "_out_stride": st})
                 assert sb.lib().sol_attn_qk_norm_rope(ctypes.byref(a)) == bad
+
+
+@pytest.mark.parametrize("change", [dict(pages=5), dict(page_size=32), dict(heads=3), dict(d=128)])
+def test_a_cache_that_is_changed_is_measured_again(sb, change):  # noqa: F811
+    """Fields set after it was made: the buffer has to hold what they say."""
+    cache = sb.make_cache(4, 16, 2, 64, device="cpu")
+    cache.c(-1)                                                           # (-1: where tensors of the CPU are)
+    for name, value in change.items():
+        setattr(cache, name, value)
+    with pytest.raises(ValueError):
+        cache.c(-1)
+    cache.data = torch.zeros(sb.sol_attn_cache_bytes(cache.pages, cache.page_size, cache.heads, cache.d), dtype=torch.uint8)
+    assert cache.c(-1)[1:5] == (cache.pages, cache.page_size, cache.heads, cache.d) and cache.bytes == cache.data.numel()
+    cache.page_size = 24
+    with pytest.raises(sb.SolAttnError):
+        cache.c(-1)
