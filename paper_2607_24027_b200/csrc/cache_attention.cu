@@ -699,7 +699,7 @@ sol_status_t check_attention(const sol_attn_cache_args* a) {
   if (!a) return SOL_ERR_INVALID_ARG;
   sol_status_t s = check(&a->cache);
   if (s != SOL_OK) return s;
-  if (a->tokens < 0 || a->requests < 0 || a->max_q <= 0 || a->max_blocks <= 0 || a->Hq <= 0) return SOL_ERR_INVALID_ARG;
+  if (a->tokens < 0 || a->requests < 0 || a->max_q < (a->tokens > 0 ? 1 : 0) || a->max_blocks <= 0 || a->Hq <= 0) return SOL_ERR_INVALID_ARG;
   if (a->type != SOL_TYPE_BF16 && a->type != SOL_TYPE_FP16) return SOL_ERR_INVALID_ARG;
   if (std::isnan(a->scale) || std::isinf(a->scale) || a->table_stride < a->max_blocks) return SOL_ERR_INVALID_ARG;
   if (a->Hq > kMaxHeads || a->Hq % a->cache.Hk) return SOL_ERR_UNSUPPORTED_SHAPE;
@@ -710,7 +710,7 @@ sol_status_t check_attention(const sol_attn_cache_args* a) {
   if (!rows_apart(a->out_stride, a->tokens, a->Hq)) return SOL_ERR_INVALID_ARG;
   if (a->requests > 0 && (!a->cu_q || !a->kv_lens || !a->block_tables)) return SOL_ERR_INVALID_ARG;
   if (!aligned(a->cu_q, 4) || !aligned(a->kv_lens, 4) || !aligned(a->block_tables, 4)) return SOL_ERR_INVALID_ARG;
-  const size_t need = sol_attn_cache_workspace_bytes(a->max_q, a->Hq, a->cache.Hk, a->cache.d);
+  const size_t need = sol_attn_cache_workspace_bytes(a->max_q > 0 ? a->max_q : 1, a->Hq, a->cache.Hk, a->cache.d);
   if (!a->workspace || !aligned(a->workspace, 1024) || a->workspace_bytes < need) return SOL_ERR_WORKSPACE;
   return SOL_OK;
 }

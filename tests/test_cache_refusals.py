@@ -45,3 +45,12 @@ def test_a_cache_that_is_changed_is_measured_again(sb, change):  # noqa: F811
     cache.page_size = 24
     with pytest.raises(sb.SolAttnError):
         cache.c(-1)
+
+
+def test_a_step_without_queries(sb):  # noqa: F811
+    """All requests idle: no rows, and a longest request of none."""
+    f = sb.lib().sol_attn_cache_attention
+    assert f(ctypes.byref(attention_args(sb, tokens=0, q=None, out=None, max_q=0))) == sb.SOL_OK
+    assert f(ctypes.byref(attention_args(sb, tokens=0, q=None, out=None, max_q=-1))) == sb.SOL_ERR_INVALID_ARG
+    assert f(ctypes.byref(attention_args(sb, max_q=0))) == sb.SOL_ERR_INVALID_ARG
+    assert f(ctypes.byref(attention_args(sb, tokens=0, q=None, out=None, max_q=0, workspace=None))) == sb.SOL_ERR_WORKSPACE
