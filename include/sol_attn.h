@@ -411,8 +411,8 @@ sol_status_t sol_attn_cache_read(const sol_attn_cache* cache /* host */, void* k
  *
  * A query that sees nothing gets zeros and lse = -inf.  The cache's values enter the products unrounded; q is scaled by a power of
  * two per row to fp16 (exact down to 2^-29 of the row's largest element); weights are rounded to fp16 (to 2^-11
- * down to 2^-25 of the row's largest; below, off by 2^-36 of it); sums are fp32 (of many queries at d = 64, a
- * quarter of the exponentials is within 2.7e-6 of its value).  Results do not depend on the order in which blocks run.  d in {64, 128}, Hq a multiple of Hk, Hq <= 1024. */
+ * down to 2^-25 of the row's largest; below, off by 2^-36 of it); sums are fp32, of the weights
+ * before that rounding.  Results do not depend on the order in which blocks run.  d in {64, 128}, Hq a multiple of Hk, Hq <= 1024. */
 typedef struct {
   const void* q; void* out; float* lse;
   int64_t q_stride[2], out_stride[2], table_stride;

@@ -11,7 +11,7 @@
 //   loader   (warp 9) the cache's units of 16 tokens into a ring of 14
 //   widen    (warps 10-15) units to fp16 tiles in a ring of four slots, K0 V0 K1 V1 ..., in the 128-byte swizzle that the tensor core reads
 // The cache's values are exact in fp16, so K and V enter the products unrounded.
-// 37 heads x 1024 queries x 32 768 keys, d = 128: 564 us, 1126 TFLOP/s; a step of 256 rows x 128 keys 2.04 us (d = 64 1.75), which is what
+// 37 heads x 1024 queries x 32 768 keys, d = 128: 545 us, 1165 TFLOP/s; a step of 256 rows x 128 keys 2.13 us (d = 64 1.78), about what
 // fwd_sm100_dense.cu takes with tiles that TMA brings: one tile's softmax, P V and Q K^T follow one another.  Tensor pipe 49 % busy.
 //
 // TMEM: S_A [0, 128)  S_B [128, 256)  O_A [256, 256 + d)  O_B [256 + d, 256 + 2 d).  Every wait is bounded.
@@ -64,6 +64,7 @@ struct Shared {
   Pieces<Tiling> pieces[kThreads / 32];          // each warp's place in the block's share: registers are scarce
   uint32_t tmem_base;
   int abort_flag;
+  int never;                                     // stays 0: the flag of waits that are not to be cut short
   int missing;                                   // a page was not there: from now on softmax looks for itself
 };
 
@@ -95,18 +96,20 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 // 2^x of two numbers up to 2^7 on the FMA pipe: x = n + f with n the nearest integer (x plus 1.5 * 2^23 rounds there), 2^f by the polynomial of
-// degree 4 whose largest relative error on [-1/2, 1/2] is least (2.6e-6, by a linear program), n added to the exponent.
+// degree 5 with constant 1 whose largest relative error on [-1/2, 1/2] is least, rounded to fp32 (1.1e-7; 1.7e-7 with the steps' roundings, as
+// good as the instruction: this goes into lse too.  Degree 4 is off by 2.6e-6), n added to the exponent.
 // Below -126 it is 2^-126.  Not for NaN.
 __device__ __forceinline__ float2 exp2_fma(float2 x) {
   x = make_float2(fmaxf(x.x, -126.f), fmaxf(x.y, -126.f));
   const float2 magic = make_float2(12582912.f, 12582912.f), minus = make_float2(-12582912.f, -12582912.f);
   const float2 t = __fadd2_rn(x, magic), n = __fadd2_rn(t, minus);
   const float2 f = __ffma2_rn(n, make_float2(-1.f, -1.f), x);
-  float2 q = make_float2(0.00956970546f, 0.00956970546f);
-  q = __ffma2_rn(q, f, make_float2(0.0559181989f, 0.0559181989f));
-  q = __ffma2_rn(q, f, make_float2(0.240247652f, 0.240247652f));
-  q = __ffma2_rn(q, f, make_float2(0.693121731f, 0.693121731f));
-  q = __ffma2_rn(q, f, make_float2(0.999999225f, 0.999999225f));
+  float2 q = make_float2(0.00132647285f, 0.00132647285f);
+  q = __ffma2_rn(q, f, make_float2(0.00967151299f, 0.00967151299f));
+  q = __ffma2_rn(q, f, make_float2(0.0555073358f, 0.0555073358f));
+  q = __ffma2_rn(q, f, make_float2(0.240222424f, 0.240222424f));
+  q = __ffma2_rn(q, f, make_float2(0.693147004f, 0.693147004f));
+  q = __ffma2_rn(q, f, make_float2(1.f, 1.f));
   return make_float2(__uint_as_float(__float_as_uint(q.x) + (__float_as_uint(t.x) << 23)),
                      __uint_as_float(__float_as_uint(q.y) + (__float_as_uint(t.y) << 23)));
 }
@@ -189,11 +192,10 @@ __device__ void loader_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at,
   // The block's shared memory must not go away under a copy, whoever ended the block and why: wait (bounded, not cut short by the flag) for
   // the last units of each lane, but for those whose place in the ring has been given to a later one (their barrier is a phase further).
   const uint32_t next = __shfl_sync(kAll, asked, (lane + kRaw) % kUnits);
-  int never = 0;
   if (lane < kUnits)
     for (uint32_t back = 1; back <= 2 && back <= asked; ++back) {
       const uint32_t x = lane + (asked - back) * kUnits;
-      if ((x + kRaw) / kUnits >= next) mbar_wait(&sm.raw_full[x % kRaw], (x / kRaw) & 1, &never);
+      if ((x + kRaw) / kUnits >= next) mbar_keep_waiting(&sm.raw_full[x % kRaw], (x / kRaw) & 1, &sm.never, kWaitCycles);
     }
 }
 static_assert(kRaw <= 2 * kUnits, "a lane's last two units are all that can be on their way");
@@ -371,8 +373,7 @@ __device__ void mma_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at, un
   // TMEM must not be released, nor shared memory go away, while MMAs use them: wait (bounded) behind everything that was issued, also if it is
   // another role that gives up, before or after this.
   if (leader) mma_commit(&sm.mma_drain);
-  int never = 0;
-  mbar_wait(&sm.mma_drain, 0, &never);
+  mbar_keep_waiting(&sm.mma_drain, 0, &sm.never, kWaitCycles);
 }
 
 template <class T, int D>
@@ -380,8 +381,8 @@ __device__ void softmax_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at
                              int warp_in_group, int lane) {
   using C = Cfg<D>;
   constexpr int kHalf = kCols / 2;
-  // With 64 channels the exponentials, not the tensor core, are what a step waits for, and a quarter of them goes to the FMA pipe: 1.75
-  // instead of 1.90 us a step.  With 128 the instructions cost more than they free: 2.27 instead of 2.06.
+  // With 64 channels the exponentials, not the tensor core, are what a step waits for, and a quarter of them goes to the FMA pipe: 1.78
+  // instead of 1.87 us a step.  With 128 the instructions cost more than they free: 2.39 instead of 2.13.
   constexpr bool kPoly = D == 64;
   const uint32_t lane_base = tmem + ((uint32_t)(warp_in_group * 32) << 16);
   const uint32_t t_s = lane_base + kTmemS + s * kCols, t_o = lane_base + kTmemO + s * D;
@@ -440,9 +441,10 @@ __device__ void softmax_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at
       tc_fence_after();
       // Columns that the row does not see are set to -inf where they lie, 16 at a time: this is rare, and as code between the loads and the
       // maxima it pushed the common path out of the instruction cache (2.63 us a step, 2.09 without it)
-      // (a vote: the loader may be setting the word, and the TMEM accesses are for whole warps)
-      const bool missing = __any_sync(kAll, *(volatile int*)&sm.missing != 0);
-      if (__any_sync(kAll, left < kCols) || missing) {
+      // (by votes: the loader may be setting the word, and the TMEM accesses are for whole warps)
+      const bool some_missing = *(volatile int*)&sm.missing != 0;
+      if (__any_sync(kAll, left < kCols || some_missing)) {
+        const bool missing = __any_sync(kAll, some_missing);
 #pragma unroll 1
         for (int x = 0; x < kUnits; ++x) {
           int seen_here = left - x * kUnit;
@@ -596,7 +598,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_chunk_kernel(cons
   unsigned char* sRaw = sKV + kSlots * C::kTileBytes;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   if (threadIdx.x == 0) {
-    sm.abort_flag = sm.missing = 0;
+    sm.abort_flag = sm.never = sm.missing = 0;
     for (int i = 0; i < kSlots; ++i) { mbar_init(&sm.kv_full[i], kUnits); mbar_init(&sm.kv_empty[i], 1); }
     for (int s = 0; s < 2; ++s) {
       mbar_init(&sm.q_full[s], 4); mbar_init(&sm.q_empty[s], 1);

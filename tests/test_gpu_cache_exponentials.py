@@ -1,0 +1,37 @@
+"""The weights of the many-row kernels by what they do to lse, where a single key has nearly all of the weight."""
+import math
+
+import pytest
+import torch
+
+from tests.test_gpu_cache import ints, sb  # noqa: F401  (sb: a fixture)
+
+pytestmark = pytest.mark.gpu
+LN2 = math.log(2)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("column", [0, 1, 2, 3, 4, 5, 6, 7])
+def test_weights_of_every_column_in_lse(sb, d, column):  # noqa: F811
+    """Two steps of 128 keys: the first sets the maximum with a logit of 0, in the second one key lies 2^1 to 2^3.9 above it, too little for a
+    new maximum; the others have no weight.  One item to a block, so that the steps are one block's.
+
+    lse = ln2 (log2(2^11 + 2^x) - 11), x = 11 + u.  Errors: x, near 16, is rounded (2^-21), u = scale q k log2(e) has two factors rounded
+    (2^-23 u); the weight 2^-22; three sums 2^-24 each; log2f is good to a unit (2^-20) and added to the maximum (2^-21); two products."""
+    rows, blocks = 64, torch.cuda.get_device_properties(0).multi_processor_count
+    cache = sb.make_cache(4, 64, 1, d)
+    k = torch.zeros(256, 1, d, dtype=torch.float16)
+    k[:, 0, 0] = -2688
+    k[5, 0, 0], k[128 + 40 + column, 0, 0] = 0, 6                         # all are values that the cache has
+    sb.sol_attn_cache_append(k.cuda(), torch.zeros_like(k).cuda(), torch.arange(256, dtype=torch.int32, device="cuda"), cache)
+    q = torch.zeros(rows * blocks, 1, d, dtype=torch.float16)
+    q[:, 0, 0] = 1 + 2.9 * torch.rand(rows * blocks, generator=torch.Generator().manual_seed(column))
+    scale = torch.tensor(LN2 / 6).item()
+    lse, out = torch.zeros(rows * blocks, 1, device="cuda"), torch.empty_like(q, device="cuda")
+    sb.sol_attn_cache_attention(q.cuda(), ints([rows * b for b in range(blocks + 1)]), ints([256] * blocks), ints([[0, 1, 2, 3]] * blocks), cache, out, rows,
+                                sb.make_cache_workspace(rows, 1, 1, d), lse=lse, causal=False, scale=scale)
+    u = scale * q[:, 0, 0].double() * 6 / LN2
+    want = torch.log1p(torch.exp2(u))
+    bound = LN2 * (2.0 ** -21 + 2.0 ** -23 * u + 2.0 ** -20 + 2.0 ** -21) + 2.0 ** -22 + 3 * 2.0 ** -24 + 2 * 2.0 ** -24 * want
+    error = (lse[:, 0].double().cpu() - want).abs()
+    assert (error <= bound).all(), ((error / bound).max().item(), error.max().item())
