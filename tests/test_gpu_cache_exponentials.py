@@ -35,3 +35,25 @@ def test_weights_of_every_column_in_lse(sb, d, column):  # noqa: F811
     bound = LN2 * (2.0 ** -21 + 2.0 ** -23 * u + 2.0 ** -20 + 2.0 ** -21) + 2.0 ** -22 + 3 * 2.0 ** -24 + 2 * 2.0 ** -24 * want
     error = (lse[:, 0].double().cpu() - want).abs()
     assert (error <= bound).all(), ((error / bound).max().item(), error.max().item())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows", [1, 12, 64])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("largest", [1.0, 1.5])
+def test_small_elements_of_a_query_are_exact(sb, dtype, rows, d, largest):  # noqa: F811
+    """An element with all of its type's bits, 2^-28 of the row's largest: a rounding in its last bit would move the logit, about 8, by 2^-12 of it.
+    lse = log(1 + exp(x)), x with an error of three roundings (2^-22) and a subtraction of 16 at most (2^-21)."""
+    cache = sb.make_cache(1, 16, 1, d)
+    k = torch.zeros(2, 1, d, dtype=torch.float16)
+    k[1, 0, 0] = 6
+    sb.sol_attn_cache_append(k.cuda(), torch.zeros_like(k).cuda(), torch.arange(2, dtype=torch.int32, device="cuda"), cache)
+    q = torch.zeros(rows, 1, d, dtype=dtype)
+    q[:, 0, d - 1] = largest * 2.0 ** 15
+    q[:, 0, 0] = 2.0 ** -13 * (2 - torch.finfo(dtype).eps)
+    scale = torch.tensor(8 / 6 * 2.0 ** 12).item()
+    lse, out = torch.zeros(rows, 1, device="cuda"), torch.empty_like(q, device="cuda")
+    sb.sol_attn_cache_attention(q.cuda(), ints([0, rows]), ints([2]), ints([[0]]), cache, out, rows, sb.make_cache_workspace(rows, 1, 1, d),
+                                lse=lse, causal=False, scale=scale)
+    x = scale * q[:, 0, 0].double() * 6
+    assert ((lse[:, 0].double().cpu() - torch.log1p(torch.exp(x))).abs() <= 2.0 ** -22 * x + 2.0 ** -18).all()
