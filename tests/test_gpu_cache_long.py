@@ -1,5 +1,4 @@
 """Attention over the cache in the state in which long calls run: blocks with ten steps and more, rings that have turned, several pieces."""
-import math
 import random
 
 import pytest
@@ -66,6 +65,38 @@ def check(sb, cache, q, cu, kv, table, causal=True, twice=True, workspace=None):
     error, bound = (lse.double() - want_lse)[some].abs(), tol_lse[some]
     assert (error <= bound).all(), (error / bound).max().item()
     return out
+
+
+def growing(sb, pages, page, Hk, d, table, kv, seed):  # noqa: F811
+    """A cache whose keys have, in 16 channels, the logarithm of n / (n - position) of their request of n: with queries of 2 there the weights grow
+    as 1 / (n - position), up to 2^14, so that maxima are replaced again and again while what was added before still counts."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    cache, n = sb.make_cache(pages, page, Hk, d), pages * page
+    k, v = (torch.randn(n, Hk, d, generator=g, device="cuda") for _ in range(2))
+    for row, m in zip(table, kv):
+        pos = torch.arange(m, device="cuda")
+        slots = torch.tensor(row, device="cuda")[pos // page] * page + pos % page
+        ramp = torch.log(m / (m - pos).float()) * d ** 0.5 / 32           # (a logit of log(n / (n - position)) with queries of 2)
+        k[slots, :, :16] = ramp[:, None, None]
+    sb.sol_attn_cache_append(k.bfloat16(), (v + 0.3).bfloat16(), torch.arange(n, dtype=torch.int32, device="cuda"), cache)
+    return cache
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("kind", list(CALLS))
+@pytest.mark.parametrize("rising", [False, True], ids=["level", "rising"])
+def test_long_calls(sb, kind, d, dtype, causal, rising):  # noqa: F811
+    requests, H, Hk = CALLS[kind]
+    kv, new = [r[0] for r in requests], [r[1] for r in requests]
+    table, cu, pages = batch(kv, new, 128, 6)
+    cache = growing(sb, pages, 128, Hk, d, table, kv, 3) if rising else filled(sb, pages, 128, Hk, d, 3)
+    q = torch.randn(cu[-1], H, d, generator=torch.Generator().manual_seed(9)) * (0.3 if rising else 1.5)
+    if rising:
+        q[..., :16] = 2
+    assert steps_of_a_block(requests, H, Hk) >= 10
+    check(sb, cache, q.to(dtype).cuda(), cu, kv, table, causal)
 
 
 @pytest.mark.parametrize("d, dtype", [(128, torch.bfloat16), (64, torch.float16)])
