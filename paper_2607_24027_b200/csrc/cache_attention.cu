@@ -461,6 +461,10 @@ struct Left {                                    // by a kernel
   int blocks, rows;                              // rows of an item
 };
 constexpr int kJoinWarps = 16;
+// Pieces of an item up to which join_wide takes the many-row kernel's.  us of a call whose 148 blocks share out items of 256 rows, wide / long, d = 64 and
+// 128: 2 pieces 22.6 / 28.4 and 30.4 / 34.6, 4 to 5 23.5 / 24.7 and 29.5 / 31.0, 10 24.5 / 29.8 and 30.8 / 35.5, 13 to 14 25.0 / 27.8 and 31.0 / 33.9,
+// 17 to 18 26.6 / 25.5 and 33.4 / 31.5, 37 31.6 / 25.3 and 38.2 / 31.5.
+constexpr int kFewPieces = 14;
 struct JoinShared {
   float joined[kJoinWarps][128 + 2];
   int counts[kJoinWarps], spans[kJoinWarps];
@@ -636,7 +640,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps, 2) cache_combine_kernel(const
     const Left& left = kernel ? many : few;
     if (left.blocks == 0) continue;
     const int2 found = pack_records(left, sh);
-    if (kernel && found.y <= 9) join_wide<T, D>(p, left, sh, found.x);
+    if (kernel && found.y <= kFewPieces) join_wide<T, D>(p, left, sh, found.x);
     else join_long<T, D>(p, left, sh, found.x, found.y);
   }
 }
