@@ -582,7 +582,10 @@ def sol_attn_cache_attention(q, cu_q, kv_lens, block_tables, cache: Cache, out, 
 
 
 def sol_attn_cache_read_status(workspace, stream=None) -> int:
-    return int(lib().sol_attn_cache_read_status(workspace.data_ptr(), _stream(stream)))
+    dev, st = _here(stream)
+    if workspace.dtype is not _U8 or workspace.get_device() != dev or workspace.numel() < 1024:
+        raise ValueError("workspace: expected the uint8 tensor of sol_attn_cache_attention on the current CUDA device")
+    return int(lib().sol_attn_cache_read_status(workspace.data_ptr(), st))
 
 
 def mask_words(n_k_blocks: int) -> int:
