@@ -50,8 +50,8 @@ struct AttnParams {
 // behind the request's first key also where the last queries are not in q, or the last keys not in the table.
 struct Request {
   int first, queries, keys, ahead;
-  // Keys that query i sees, causal: ahead + i + 1, at least 0 (~i is -i - 1; the sum fits in 32 bits without a sign).
-  __device__ int sees(int i) const { return ahead < ~i ? 0 : (int)min((uint32_t)keys, (uint32_t)ahead + (uint32_t)i + 1u); }
+  // Keys that query i sees, causal.
+  __device__ int sees(int i) const { return (int)max(0LL, min((long long)keys, (long long)ahead + i + 1)); }
 };
 __device__ __forceinline__ Request request_at(const AttnParams& p, int b) {
   const int end = p.cu_q[b + 1];

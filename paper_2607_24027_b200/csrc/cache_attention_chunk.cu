@@ -64,7 +64,6 @@ struct Shared {
   Pieces<Tiling> pieces[kThreads / 32];          // each warp's place in the block's share: registers are scarce
   uint32_t tmem_base;
   int abort_flag;
-  int never;                                     // stays 0: the flag of waits that are not to be cut short
   int missing;                                   // a page was not there: from now on softmax looks for itself
 };
 
@@ -191,11 +190,12 @@ __device__ void loader_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at,
   if (!ok && lane == 0) flag_timeout(sm, p);
   // The block's shared memory must not go away under a copy, whoever ended the block and why: wait (bounded, not cut short by the flag) for
   // the last units of each lane, but for those whose place in the ring has been given to a later one (their barrier is a phase further).
+  int never = 0;
   const uint32_t next = __shfl_sync(kAll, asked, (lane + kRaw) % kUnits);
   if (lane < kUnits)
     for (uint32_t back = 1; back <= 2 && back <= asked; ++back) {
       const uint32_t x = lane + (asked - back) * kUnits;
-      if ((x + kRaw) / kUnits >= next) mbar_keep_waiting(&sm.raw_full[x % kRaw], (x / kRaw) & 1, &sm.never, kWaitCycles);
+      if ((x + kRaw) / kUnits >= next) mbar_wait(&sm.raw_full[x % kRaw], (x / kRaw) & 1, &never);
     }
 }
 static_assert(kRaw <= 2 * kUnits, "a lane's last two units are all that can be on their way");
@@ -372,8 +372,9 @@ __device__ void mma_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at, un
   __syncwarp();
   // TMEM must not be released, nor shared memory go away, while MMAs use them: wait (bounded) behind everything that was issued, also if it is
   // another role that gives up, before or after this.
+  int never = 0;
   if (leader) mma_commit(&sm.mma_drain);
-  mbar_keep_waiting(&sm.mma_drain, 0, &sm.never, kWaitCycles);
+  mbar_wait(&sm.mma_drain, 0, &never);
 }
 
 template <class T, int D>
@@ -442,9 +443,8 @@ __device__ void softmax_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at
       // Columns that the row does not see are set to -inf where they lie, 16 at a time: this is rare, and as code between the loads and the
       // maxima it pushed the common path out of the instruction cache (2.63 us a step, 2.09 without it)
       // (by votes: the loader may be setting the word, and the TMEM accesses are for whole warps)
-      const bool some_missing = *(volatile int*)&sm.missing != 0;
-      if (__any_sync(kAll, left < kCols || some_missing)) {
-        const bool missing = __any_sync(kAll, some_missing);
+      const bool missing = __any_sync(kAll, *(volatile int*)&sm.missing != 0);
+      if (__any_sync(kAll, left < kCols) || missing) {
 #pragma unroll 1
         for (int x = 0; x < kUnits; ++x) {
           int seen_here = left - x * kUnit;
@@ -598,7 +598,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_attention_chunk_kernel(cons
   unsigned char* sRaw = sKV + kSlots * C::kTileBytes;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   if (threadIdx.x == 0) {
-    sm.abort_flag = sm.never = sm.missing = 0;
+    sm.abort_flag = sm.missing = 0;
     for (int i = 0; i < kSlots; ++i) { mbar_init(&sm.kv_full[i], kUnits); mbar_init(&sm.kv_empty[i], 1); }
     for (int s = 0; s < 2; ++s) {
       mbar_init(&sm.q_full[s], 4); mbar_init(&sm.q_empty[s], 1);
