@@ -409,7 +409,7 @@ sol_status_t sol_attn_cache_read(const sol_attn_cache* cache /* host */, void* k
  *   workspace    sol_attn_cache_workspace_bytes(), 1024-byte aligned, zeroed once before its first use; overwritten by every call,
  *                so calls that share one and overlap on the GPU race
  *
- * A query that sees nothing gets zeros and lse = -inf.  The cache's values enter the products unrounded; q is scaled by a power of
+ * A query that sees nothing gets zeros and lse = -inf.  Logits are fp32 numbers: one above their range makes its row NaN, one below has no weight.  The cache's values enter the products unrounded; q is scaled by a power of
  * two per row to fp16 (exact down to 2^-28 of the row's largest element); weights are rounded to fp16 (to 2^-11
  * down to 2^-25 of the row's largest; below, off by 2^-36 of it); sums are fp32, of the weights
  * before that rounding.  Results do not depend on the order in which blocks run.  d in {64, 128}, Hq a multiple of Hk, Hq <= 1024. */

@@ -500,6 +500,7 @@ __device__ void softmax_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at
           }
         }
         l *= f;
+        if (mx == INFINITY) l = NAN;             // (a logit above fp32's range: with nm = -inf all weights would be 0)
         nm = nm_new;
         seen = seen || some;
       }

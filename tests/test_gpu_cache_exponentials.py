@@ -57,3 +57,31 @@ def test_small_elements_of_a_query_are_exact(sb, dtype, rows, d, largest):  # no
                                 lse=lse, causal=False, scale=scale)
     x = scale * q[:, 0, 0].double() * 6
     assert ((lse[:, 0].double().cpu() - torch.log1p(torch.exp(x))).abs() <= 2.0 ** -22 * x + 2.0 ** -18).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows", [1, 12, 64])
+@pytest.mark.parametrize("keys", [3, 300, 5000])
+def test_logits_outside_fp32(sb, d, rows, keys):  # noqa: F811
+    """A logit of 1e40 makes its row NaN, one of -1e40 has no weight; the rows beside it are exact."""
+    n, key = -(-keys // 64), keys * 2 // 3
+    cache = sb.make_cache(n, 64, 1, d)
+    k, v = torch.zeros(keys, 1, d, dtype=torch.bfloat16), torch.randn(keys, 1, d, generator=torch.Generator().manual_seed(1)).bfloat16()
+    k[key, 0, 0], k[key, 0, 1] = 2688, -2688
+    slots = torch.arange(keys, dtype=torch.int32, device="cuda")
+    sb.sol_attn_cache_append(k.cuda(), v.cuda(), slots, cache)
+    held = torch.empty_like(v, device="cuda")
+    sb.sol_attn_cache_read(cache, slots, None, held)
+    q = torch.zeros(rows, 3, d, dtype=torch.bfloat16)
+    q[:, 1, 0], q[:, 2, 1] = 2.0 ** 126, 2.0 ** 126
+    lse, out = torch.zeros(rows, 3, device="cuda"), torch.empty_like(q, device="cuda")
+    sb.sol_attn_cache_attention(q.cuda(), ints([0, rows]), ints([keys]), ints([list(range(n))]), cache, out, rows,
+                                sb.make_cache_workspace(rows, 3, 1, d), lse=lse, causal=False, scale=1.0)
+    assert out[:, 1].isnan().all() and lse[:, 1].isnan().all()
+    others = held[torch.arange(keys) != key].double()
+    for head, values in ((0, held.double()), (2, others)):
+        want = values.mean(0)
+        # weights are all alike: what is left are the sum's, the products' and the result's roundings
+        bound = 2.0 ** -8 * want.abs() + 2.0 ** -11 * values.abs().mean(0)
+        assert ((out[:, head].double() - want).abs() <= bound).all(), head
+        assert ((lse[:, head].double() - math.log(len(values))).abs() <= 2.0 ** -18).all(), head
