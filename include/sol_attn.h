@@ -349,7 +349,7 @@ sol_status_t sol_attn_block_tables(const sol_attn_tables_args* args /* host */);
  *   positions            int32 [batch][tokens]; NULL: the index of the token in its batch.  A token whose position is not in
  *                        [0, table_rows) is left out: its rows of the outputs are left as they were (padding)
  *
- * d in {64, 128}; rot a multiple of 16 up to d.  Reads and writes every element once. */
+ * With rot = 0 positions are not looked at.  d in {64, 128}; rot a multiple of 16 up to d.  Reads and writes every element once. */
 typedef struct {
   const void* q; const void* k; void* q_out; void* k_out;
   int64_t q_stride[3], k_stride[3], q_out_stride[3], k_out_stride[3];
@@ -409,10 +409,11 @@ sol_status_t sol_attn_cache_read(const sol_attn_cache* cache /* host */, void* k
  *   workspace    sol_attn_cache_workspace_bytes(), 1024-byte aligned, zeroed once before its first use; overwritten by every call,
  *                so calls that share one and overlap on the GPU race
  *
- * A query that sees nothing gets zeros and lse = -inf.  Logits are fp32 numbers: one above their range makes its row NaN, one below has no weight.  The cache's values enter the products unrounded; q is scaled by a power of
- * two per row to fp16 (exact down to 2^-28 of the row's largest element); weights are rounded to fp16 (to 2^-11
- * down to 2^-25 of the row's largest; below, off by 2^-36 of it); sums are fp32, of the weights
- * before that rounding.  Results do not depend on the order in which blocks run.  d in {64, 128}, Hq a multiple of Hk, Hq <= 1024. */
+ * A query that sees nothing gets zeros and lse = -inf.  Logits are fp32 numbers: one above their range makes its row NaN, one below has no
+ * weight.  The cache's values enter the products unrounded; q is scaled by a power of two per row to fp16 (exact down to 2^-28 of the
+ * row's largest element); weights are rounded to fp16 (to 2^-11 down to 2^-25 of the row's largest; below, off by 2^-36 of it); sums
+ * are fp32, of the weights before that rounding.  Results do not depend on the order in which blocks run.  d in {64, 128}, Hq a
+ * multiple of Hk, Hq <= 1024. */
 typedef struct {
   const void* q; void* out; float* lse;
   int64_t q_stride[2], out_stride[2], table_stride;

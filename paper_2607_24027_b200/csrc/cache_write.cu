@@ -67,7 +67,9 @@ __device__ __forceinline__ uint2 codes_of(const uint32_t* w, uint32_t most16, fl
   float2 y[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) y[i] = __ffma2_rn(Two<T>::widen(w[i]), inv2, zero2);
-  if (most > 6.5f * 448.f) {                     // only then a quotient may pass 7, and much further
+  // A quotient is 7 at most with a scale of full precision, less than 9 with a subnormal one (the scale 2^-9 stands for up to 1.5 times itself), which
+  // the splitting takes and the conversion makes 6.  Only where the scale is at its end may it be anything, up to an infinity.
+  if (most > 6.5f * 448.f) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = make_float2(fminf(fmaxf(y[i].x, -8.f), 8.f), fminf(fmaxf(y[i].y, -8.f), 8.f));
   }
