@@ -4,8 +4,8 @@
 // tokens, so every block forms both sums for itself and fills the tokens that it owns: one launch, no block waits for
 // another.  A page is entered in its request's table by the thread of the first token that it holds; those of tokens behind max_tokens, which
 // have no thread, by the first block.
-// Bound by latency: lengths, two barriers, the free list.  64 requests with a token each 3.3 us in a graph, 192 with 196 000 tokens 6.3
-// (2.9 and 5.6 without the look at the pages that are taken).
+// Bound by latency: lengths, two barriers, the free list.  64 requests with a token each 3.1 us in a graph, 192 with 196 000 tokens 6.2
+// (2.8 and 5.5 without the look at the pages that are taken).
 #include "cache.cuh"
 
 namespace sol {

@@ -190,15 +190,16 @@ __device__ void loader_role(Shared& sm, const AttnParams& p, Pieces<Tiling>& at,
   if (!ok && lane == 0) flag_timeout(sm, p);
   // The block's shared memory must not go away under a copy, whoever ended the block and why: wait (bounded, not cut short by the flag) for
   // the last units of each lane, but for those whose place in the ring has been given to a later one (their barrier is a phase further).
+  // (Three: a lane may be a unit ahead of the others, and then its last but two may have the ring's place still.)
   int never = 0;
   const uint32_t next = __shfl_sync(kAll, asked, (lane + kRaw) % kUnits);
   if (lane < kUnits)
-    for (uint32_t back = 1; back <= 2 && back <= asked; ++back) {
+    for (uint32_t back = 1; back <= 3 && back <= asked; ++back) {
       const uint32_t x = lane + (asked - back) * kUnits;
       if ((x + kRaw) / kUnits >= next) mbar_wait(&sm.raw_full[x % kRaw], (x / kRaw) & 1, &never);
     }
 }
-static_assert(kRaw <= 2 * kUnits, "a lane's last two units are all that can be on their way");
+static_assert(kRaw <= 2 * kUnits, "a lane's last three units are all that can be on their way");
 
 // Raw units to fp16 tiles.  The tasks, eight units of keys and eight of values for each tile of keys, lie one after the other, and
 // kWideners warps take them in turn.
